@@ -61,30 +61,32 @@ bool overlap(const Matrix &a, const Matrix &b)
 struct Checker {
     Matrix m[16];
     int n = 0;
+    int twin_in = -1, twin_out = -1;      // places of an input and of the output that may coincide with it exactly
     ssd_status st = SSD_OK;
 
-    void add(const void *p, int64_t ld, int64_t rows, int64_t cols, int esize, bool write, bool needed)
+    // The argument's place in `m`, or -1 where there is none.
+    int add(const void *p, int64_t ld, int64_t rows, int64_t cols, int esize, bool write, bool needed)
     {
         if (!p && rows > 0 && needed) st = SSD_ERR_ARG;
-        if (!p || rows == 0) return;
+        if (!p || rows == 0) return -1;
         if (rows > 1 && (ld < cols || ld >= (int64_t(1) << 36))) {
             st = SSD_ERR_ARG;
-            return;
+            return -1;
         }
         if (st == SSD_OK && addr(p) % esize) st = SSD_ERR_ALIGN;
-        m[n++] = Matrix{const_cast<void *>(p), ld, rows, cols, esize, write};
+        m[n] = Matrix{const_cast<void *>(p), ld, rows, cols, esize, write};
+        return n++;
     }
-    // `twin`: index of an input that output `of` may coincide with exactly
-    ssd_status overlaps(const void *workspace, int64_t bytes, const void *twin_in, const void *twin_out) const
+    ssd_status overlaps(const void *workspace, int64_t bytes) const
     {
         for (int i = 0; i < n; ++i) {
             if (bytes > 0 && overlap(m[i], Matrix{const_cast<void *>(workspace), bytes, 1, bytes, 1, true})) return SSD_ERR_ARG;
             for (int j = 0; j < i; ++j) {
                 if (!m[i].write && !m[j].write) continue;
                 if (!overlap(m[i], m[j])) continue;
-                const bool same = m[i].p == m[j].p && m[i].ld == m[j].ld;
-                const bool pair = (m[i].p == twin_in && m[j].p == twin_out) && m[i].write != m[j].write;
-                if (twin_in && twin_in == twin_out && same && pair) continue;
+                // by their places: another argument may have the same address and pitch
+                const bool twins = (i == twin_out && j == twin_in) || (i == twin_in && j == twin_out);
+                if (twins && m[i].p == m[j].p && m[i].ld == m[j].ld) continue;
                 return SSD_ERR_ARG;
             }
         }
@@ -457,8 +459,8 @@ ssd_status check(const ssd_linear_fwd *a, Forward *f, Checker *k)
     k->add(a->x, a->ldx, f->rows, f->in, es, false, true);
     k->add(a->weight, a->ldw, f->out, f->in, es, false, true);
     k->add(a->bias, f->out, 1, f->out, 4, false, false);
-    k->add(a->residual, a->ldr, f->rows, f->out, es, false, false);
-    k->add(a->y, a->ldy, f->rows, f->out, es, true, true);
+    k->twin_in = k->add(a->residual, a->ldr, f->rows, f->out, es, false, false);
+    k->twin_out = k->add(a->y, a->ldy, f->rows, f->out, es, true, true);
     k->add(a->z, a->ldz, f->rows, f->out, es, true, false);
     f->e.bias[0] = a->bias;
     f->e.residual = a->residual;
@@ -557,7 +559,7 @@ template <typename Work, typename Args> ssd_status workspace_of(const Args *args
 }
 
 template <typename Work, typename Args>
-ssd_status run_call(const Args *args, void *workspace, int64_t workspace_bytes, void *cuda_stream, const void *twin_in, const void *twin_out)
+ssd_status run_call(const Args *args, void *workspace, int64_t workspace_bytes, void *cuda_stream)
 {
     Work w;
     Checker k;
@@ -567,7 +569,7 @@ ssd_status run_call(const Args *args, void *workspace, int64_t workspace_bytes, 
     run(count, w);
     if (count.used > 0 && (!workspace || workspace_bytes < count.used)) return SSD_ERR_ARG;
     if (count.used > 0 && addr(workspace) % 16) return SSD_ERR_ALIGN;
-    st = k.overlaps(workspace, count.used, twin_in, twin_out);
+    st = k.overlaps(workspace, count.used);
     if (st != SSD_OK) return st;
     Call c;
     static unsigned char none;
@@ -588,19 +590,19 @@ ssd_status ssd_gated_backward_workspace(const ssd_gated_bwd *args, int64_t *byte
 
 ssd_status ssd_linear_forward(const ssd_linear_fwd *args, void *workspace, int64_t workspace_bytes, void *cuda_stream)
 {
-    return run_call<Forward>(args, workspace, workspace_bytes, cuda_stream, args ? args->residual : nullptr, args ? args->y : nullptr);
+    return run_call<Forward>(args, workspace, workspace_bytes, cuda_stream);
 }
 ssd_status ssd_linear_backward(const ssd_linear_bwd *args, void *workspace, int64_t workspace_bytes, void *cuda_stream)
 {
-    return run_call<Backward>(args, workspace, workspace_bytes, cuda_stream, nullptr, nullptr);
+    return run_call<Backward>(args, workspace, workspace_bytes, cuda_stream);
 }
 ssd_status ssd_gated_forward(const ssd_gated_fwd *args, void *workspace, int64_t workspace_bytes, void *cuda_stream)
 {
-    return run_call<Forward>(args, workspace, workspace_bytes, cuda_stream, nullptr, nullptr);
+    return run_call<Forward>(args, workspace, workspace_bytes, cuda_stream);
 }
 ssd_status ssd_gated_backward(const ssd_gated_bwd *args, void *workspace, int64_t workspace_bytes, void *cuda_stream)
 {
-    return run_call<Backward>(args, workspace, workspace_bytes, cuda_stream, nullptr, nullptr);
+    return run_call<Backward>(args, workspace, workspace_bytes, cuda_stream);
 }
 
 ssd_status ssd_layer_error(int32_t *flag)

@@ -1,0 +1,33 @@
+"""Calls of the layer operators that are refused although every argument by itself is a good one.  No GPU: nothing is enqueued."""
+import ctypes as C
+
+import pytest
+
+from paper_2012_05396_b200 import binding as B
+from paper_2012_05396_b200 import build as libbuild
+from paper_2012_05396_b200 import layers as L
+from tests.test_layers_abi import args_of, status
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    libbuild.build_library()
+
+
+@pytest.mark.parametrize("dtype", [B.SSD_BF16, B.SSD_F32])
+@pytest.mark.parametrize("victim", ["x", "weight"])
+@pytest.mark.parametrize("rows", [8, 64])
+def test_only_the_residual_may_be_the_result(rows, victim, dtype):
+    """A result over its residual is allowed; over another input that is the residual too it is not (x = act(x W^T) + x in place)."""
+    a = args_of("linear_forward", rows=rows, in_features=64, out_features=64, dtype=dtype, **{n: 64 for n, t in L.ssd_linear_fwd._fields_ if n.startswith("ld")})
+    if victim == "weight":
+        a.rows = 64
+    p = getattr(a, victim)
+    a.residual = a.y = p
+    assert status("linear_forward", a) == B.SSD_ERR_ARG
+    a.z = None
+    assert status("linear_forward", a) == B.SSD_ERR_ARG
+    # and the same of a vector that the result lies over
+    a = args_of("linear_forward", rows=1, in_features=64, out_features=64, dtype=B.SSD_F32, **{n: 64 for n, t in L.ssd_linear_fwd._fields_ if n.startswith("ld")})
+    a.residual = a.y = a.bias
+    assert status("linear_forward", a) == B.SSD_ERR_ARG
