@@ -86,7 +86,7 @@ struct Checker {
                 if (!overlap(m[i], m[j])) continue;
                 // by their places: another argument may have the same address and pitch
                 const bool twins = (i == twin_out && j == twin_in) || (i == twin_in && j == twin_out);
-                if (twins && m[i].p == m[j].p && m[i].ld == m[j].ld) continue;
+                if (twins && m[i].p == m[j].p && (m[i].ld == m[j].ld || m[i].rows == 1)) continue;
                 return SSD_ERR_ARG;
             }
         }
