@@ -124,8 +124,13 @@ struct Backward {
 // Work of a call.  The same code runs twice: once without a workspace, to count the bytes it takes from it, and once
 // in earnest.
 
+// What a call takes from its workspace starts on 32 bytes (sums of split products go out by 256-bit stores), the workspace itself on 16: the
+// room to round it up is counted with the rest.
+constexpr int64_t kWorkspaceAlign = 16, kTakeAlign = 32;
+int64_t workspace_bytes_of(int64_t used) { return used ? used + (kTakeAlign - kWorkspaceAlign) : 0; }
+
 struct Call {
-    unsigned char *base = nullptr;      // NULL: count only
+    unsigned char *base = nullptr;      // a multiple of kTakeAlign; NULL: count only
     int64_t used = 0;
     cudaStream_t stream = nullptr;
     cudaError_t err = cudaSuccess;
@@ -554,7 +559,7 @@ template <typename Work, typename Args> ssd_status workspace_of(const Args *args
     if (st != SSD_OK) return st;
     Call c;
     run(c, w);
-    *bytes = c.used;
+    *bytes = workspace_bytes_of(c.used);
     return SSD_OK;
 }
 
@@ -567,13 +572,14 @@ ssd_status run_call(const Args *args, void *workspace, int64_t workspace_bytes, 
     if (st != SSD_OK) return st;
     Call count;
     run(count, w);
-    if (count.used > 0 && (!workspace || workspace_bytes < count.used)) return SSD_ERR_ARG;
-    if (count.used > 0 && addr(workspace) % 16) return SSD_ERR_ALIGN;
-    st = k.overlaps(workspace, count.used);
+    const int64_t need = workspace_bytes_of(count.used);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return SSD_ERR_ARG;
+    if (need > 0 && addr(workspace) % kWorkspaceAlign) return SSD_ERR_ALIGN;
+    st = k.overlaps(workspace, need);
     if (st != SSD_OK) return st;
     Call c;
-    static unsigned char none;
-    c.base = count.used > 0 ? static_cast<unsigned char *>(workspace) : &none;
+    alignas(kTakeAlign) static unsigned char none;
+    c.base = need > 0 ? static_cast<unsigned char *>(workspace) + (addr(workspace) % kTakeAlign ? kTakeAlign - kWorkspaceAlign : 0) : &none;
     c.stream = static_cast<cudaStream_t>(cuda_stream);
     run(c, w);
     return c.err == cudaSuccess ? SSD_OK : layer_cuda_fail(c.err);

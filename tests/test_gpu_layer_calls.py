@@ -22,3 +22,56 @@ def test_one_row_over_its_residual_whatever_the_pitches(dtype):
     a = L.ssd_linear_fwd(1, 72, 40, code, L.SSD_ACT_GELU, x.data_ptr(), 0, w.data_ptr(), 72, None, r.data_ptr(), 40, r.data_ptr(), 1000)
     assert L.lib().ssd_linear_forward(C.byref(a), None, 0, torch.cuda.current_stream().cuda_stream) == B.SSD_OK
     check(r, ref["y"], "y over its residual")
+
+
+# Calls that take every kind of room from a workspace, (op, rows, in, out, dtype): sums of a contraction split over pairs, and over pairs for weight
+# gradients; operands in parts; rows that are copied; column sums; strips of dx of a few rows.
+ROOM = [("linear_forward", 256, 25088, 4096, "bf16"), ("linear_forward", 300, 4001, 600, "bf16"), ("linear_forward", 260, 2048, 1000, "f32"),
+        ("gated_forward", 300, 2100, 500, "bf16"), ("gated_forward", 256, 1024, 512, "f32"), ("linear_backward", 256, 4096, 1000, "f32"),
+        ("linear_backward", 2000, 600, 700, "bf16"), ("gated_backward", 300, 520, 700, "f32"), ("gated_backward", 1100, 264, 333, "bf16"),
+        ("linear_backward", 7, 500, 900, "f32")]
+
+
+@pytest.mark.parametrize("at", [0, 16, 48, 112])
+@pytest.mark.parametrize("case", ROOM, ids=str)
+def test_workspaces_on_any_16_bytes(case, at):
+    """Exactly the bytes that were asked for, on an odd multiple of 16: the same bits as anywhere else, and nothing written beside them."""
+    op, rows, d, f, dtype = case
+    g, t = gen(2), DT[dtype]
+    code = B.SSD_F32 if dtype == "f32" else B.SSD_BF16
+    x, w, w2 = normal(g, rows, d, dtype=t), normal(g, f, d, dtype=t, std=d ** -0.5), normal(g, f, d, dtype=t, std=d ** -0.5)
+    dy, z, u = (normal(g, rows, f, dtype=t) for _ in range(3))
+
+    def empty(*shape, dt=t):
+        return torch.empty(*shape, device="cuda", dtype=dt)
+
+    if op == "linear_forward":
+        outs = [empty(rows, f)]
+        a = L.ssd_linear_fwd(rows, d, f, code, 2, x.data_ptr(), d, w.data_ptr(), d, None, None, 0, outs[0].data_ptr(), f)
+        want = L.ssd_linear_forward(x, w, act=2)[:1]
+    elif op == "gated_forward":
+        outs = [empty(rows, f)]
+        a = L.ssd_gated_fwd(rows, d, f, code, 3, x.data_ptr(), d, w.data_ptr(), d, w2.data_ptr(), d, None, None, outs[0].data_ptr(), f)
+        want = L.ssd_gated_forward(x, w, w2)[:1]
+    elif op == "linear_backward":
+        outs = [empty(rows, d), empty(f, d, dt=torch.float32), empty(f, dt=torch.float32)]
+        a = L.ssd_linear_bwd(rows, d, f, code, 2, B.SSD_F32, 0, dy.data_ptr(), f, x.data_ptr(), d, w.data_ptr(), d, z.data_ptr(), f, outs[0].data_ptr(), d,
+                             outs[1].data_ptr(), d, outs[2].data_ptr())
+        want = L.ssd_linear_backward(dy, x, w, z, act=2)
+    else:
+        outs = [empty(rows, d), empty(f, d, dt=torch.float32), empty(f, d, dt=torch.float32), empty(f, dt=torch.float32), empty(f, dt=torch.float32)]
+        a = L.ssd_gated_bwd(rows, d, f, code, 3, B.SSD_F32, 0, dy.data_ptr(), f, x.data_ptr(), d, w.data_ptr(), d, w2.data_ptr(), d, z.data_ptr(), f,
+                            u.data_ptr(), f, outs[0].data_ptr(), d, outs[1].data_ptr(), d, outs[2].data_ptr(), d, outs[3].data_ptr(), outs[4].data_ptr())
+        want = L.ssd_gated_backward(dy, x, w, w2, z, u)
+    n = C.c_int64()
+    assert getattr(L.lib(), f"ssd_{op}_workspace")(C.byref(a), C.byref(n)) == B.SSD_OK and n.value > 0
+    room = torch.full((n.value + 256,), 0x5A, device="cuda", dtype=torch.uint8)
+    assert room.data_ptr() % 32 == 0
+    assert getattr(L.lib(), f"ssd_{op}")(C.byref(a), room.data_ptr() + at, n.value, torch.cuda.current_stream().cuda_stream) == B.SSD_OK
+    assert all(torch.equal(p, q) for p, q in zip(outs, want))
+    assert bool((room[:at] == 0x5A).all()) and bool((room[at + n.value:] == 0x5A).all())
+    # and the same through the torch interface
+    if op == "linear_forward":
+        assert torch.equal(L.ssd_linear_forward(x, w, act=2, workspace=room[at:at + n.value])[0], want[0])
+        with pytest.raises(B.SsdError):
+            L.ssd_linear_forward(x, w, act=2, workspace=room[at:at + n.value - 1])

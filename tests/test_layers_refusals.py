@@ -6,7 +6,7 @@ import pytest
 from paper_2012_05396_b200 import binding as B
 from paper_2012_05396_b200 import build as libbuild
 from paper_2012_05396_b200 import layers as L
-from tests.test_layers_abi import args_of, status
+from tests.test_layers_abi import BASE, STEP, args_of, large, need, status
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -31,3 +31,13 @@ def test_only_the_residual_may_be_the_result(rows, victim, dtype):
     a = args_of("linear_forward", rows=1, in_features=64, out_features=64, dtype=B.SSD_F32, **{n: 64 for n, t in L.ssd_linear_fwd._fields_ if n.startswith("ld")})
     a.residual = a.y = a.bias
     assert status("linear_forward", a) == B.SSD_ERR_ARG
+
+
+@pytest.mark.parametrize("op", ["linear_forward", "linear_backward", "gated_forward", "gated_backward"])
+def test_workspaces_count_the_room_to_align_them(op):
+    """A workspace may start on any 16 bytes; what calls take from it are multiples of 256 bytes on 32, so 16 more are asked for."""
+    st, n = need(op, large(op, dtype=B.SSD_F32))
+    assert st == B.SSD_OK and n > 0 and n % 256 == 16
+    for at in (0, 16):
+        assert status(op, large(op, dtype=B.SSD_F32), workspace=BASE + 100 * STEP + at, size=n - 1) == B.SSD_ERR_ARG
+        assert status(op, large(op, dtype=B.SSD_F32), workspace=BASE + 100 * STEP + at + 8, size=n + 64) == B.SSD_ERR_ALIGN
