@@ -313,7 +313,7 @@ void run_forward(Call &c, const Forward &f)
 {
     if (f.rows == 0) return;
     if (few_rows(f)) {
-        RowsForward q{f.x, {f.w[0], f.w[1]}, f.ldx, {f.ldw[0], f.ldw[1]}, int(f.rows), int(f.in), int(f.out), f.mats == 2, 0, f.e};
+        RowsForward q{f.x, {f.w[0], f.w[1]}, f.ldx, {f.ldw[0], f.ldw[1]}, int(f.rows), int(f.in), int(f.out), f.mats == 2, 0, 0, f.e};
         if (c.live()) {
             const cudaError_t e = launch_rows_forward(q, c.stream);
             if (c.err == cudaSuccess) c.err = e;

@@ -68,7 +68,8 @@ cudaError_t launch_product(const Product &p, float *partial, cudaStream_t stream
 struct RowsForward {
     const void *x, *w[2];
     int64_t ldx, ldw[2];
-    int rows, in, out, gated, slices;
+    int rows, in, out, gated;
+    int slices, across;                  // set by the launcher: warps that share a contraction, blocks over the weight rows
     Epilogue e;
 };
 

@@ -75,8 +75,8 @@ template <typename T, bool VEC, int R, bool GATED> __global__ void __launch_boun
     dependents_may_start();
     wait_for_previous();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int per_block = kWarps / p.slices, slice = warp % p.slices;
-    const int n0 = (int(blockIdx.x) * per_block + warp / p.slices) * kOuts;
+    const int per_block = kWarps / p.slices, slice = warp % p.slices, across = int(blockIdx.x % unsigned(p.across));
+    const int n0 = (across * per_block + warp / p.slices) * kOuts;
     const T *wrow[kWarpRows];
     bool in[kWarpRows];
 #pragma unroll
@@ -88,8 +88,8 @@ template <typename T, bool VEC, int R, bool GATED> __global__ void __launch_boun
     float acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.0f;
-    // R rows of x for the blocks of each y
-    const int r0 = int(blockIdx.y) * R, rows = p.rows - r0 < R ? p.rows - r0 : R;
+    // R rows of x for every `across` blocks
+    const int r0 = int(blockIdx.x / unsigned(p.across)) * R, rows = p.rows - r0 < R ? p.rows - r0 : R;
     const T *x = static_cast<const T *>(p.x) + r0 * p.ldx;
     // two steps of 256 of the contraction under way at a time (one where the registers are wanted for the sums)
     constexpr int kSteps = R <= 4 ? 2 : 1;
@@ -122,7 +122,7 @@ template <typename T, bool VEC, int R, bool GATED> __global__ void __launch_boun
     // one thread for each output of the block
     for (int t = threadIdx.x; t < per_block * kOuts * R; t += kThreads) {
         const int g = t / (kOuts * R), i = t / R % kOuts, r = t % R;
-        const int n = (int(blockIdx.x) * per_block + g) * kOuts + i;
+        const int n = (across * per_block + g) * kOuts + i;
         if (n >= p.out || r >= rows) continue;
         float v = 0.0f, u = 0.0f;
         for (int s = 0; s < p.slices; ++s) {
@@ -387,8 +387,9 @@ template <typename Kernel> cudaError_t launch_slices(Kernel kernel, RowsForward 
     p.slices = 1;
     while (p.slices < kWarps && blocks(2 * p.slices) <= resident && p.in > step * p.slices) p.slices *= 2;
     const int64_t count = (groups + kWarps / p.slices - 1) / (kWarps / p.slices);
-    if (count > INT32_MAX) return cudaErrorInvalidConfiguration;
-    return launch(kernel, dim3(unsigned(count), unsigned((p.rows + rows - 1) / rows)), kThreads, 0, 1, stream, p);
+    if (count * times > INT32_MAX) return cudaErrorInvalidConfiguration;
+    p.across = int(count);
+    return launch(kernel, dim3(unsigned(count * times)), kThreads, 0, 1, stream, p);      // in one dimension: the others end at 65535 blocks
 }
 
 template <typename T, bool VEC, int R> cudaError_t launch_forward(const RowsForward &p, cudaStream_t stream)

@@ -75,3 +75,20 @@ def test_workspaces_on_any_16_bytes(case, at):
         assert torch.equal(L.ssd_linear_forward(x, w, act=2, workspace=room[at:at + n.value])[0], want[0])
         with pytest.raises(B.SsdError):
             L.ssd_linear_forward(x, w, act=2, workspace=room[at:at + n.value - 1])
+
+
+@pytest.mark.parametrize("rows", [65535 * 8, 65535 * 8 + 1, 600000, 1048577])
+@pytest.mark.parametrize("width", [(8, 8), (3, 5), (10, 10)], ids=str)
+def test_more_rows_than_a_grid_is_high(rows, width):
+    """Small float32 layers over very many rows: eight rows a block, and a grid is at most 65535 blocks high."""
+    g, (d, f) = gen(3), width
+    x, w, w2 = normal(g, rows, d, dtype=torch.float32), normal(g, f, d, dtype=torch.float32), normal(g, f, d, dtype=torch.float32)
+    b, r = normal(g, f, dtype=torch.float32), normal(g, rows, f, dtype=torch.float32)
+    y, z = L.ssd_linear_forward(x, w, bias=b, residual=r, act=2, keep=True)
+    ref = R.linear_forward(x, w, b, r, 2)
+    check(y, ref["y"], "y")
+    check(z, ref["z"], "z")
+    h, gate, up = L.ssd_gated_forward(x, w, w2, b, keep=True)
+    ref = R.gated_forward(x, w, w2, b, None, 3)
+    for got, k in ((h, "h"), (gate, "gate"), (up, "up")):
+        check(got, ref[k], k)
