@@ -374,34 +374,38 @@ bool aligned(const void *p, int64_t ld, int rows, int size, int to) { return rei
 // The contraction is shared by as many warps as still fit the chip in one go: too few leave its memory idle, and what does not fit
 // runs after the rest.
 // `rows`: rows of x of a block; `group`: weight rows of a warp, over both matrices; `step`: contraction that a warp takes at a time.
-template <typename Kernel> cudaError_t launch_slices(Kernel kernel, RowsForward p, int rows, int group, int step, cudaStream_t stream)
+// The kernel is a template argument, not a function argument: all of them have one type, and each has to be asked for its own occupancy, so that
+// the split, and with it the order of the sums, follows from the call alone.  (It is the same on every device that this code runs on.)
+template <void (*KERNEL)(RowsForward)> cudaError_t launch_slices(RowsForward p, int rows, int group, int step, cudaStream_t stream)
 {
-    static const int resident = [&] {
-        int fit = 0;
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, kernel, kThreads, 0) != cudaSuccess || fit < 1) fit = 1;
-        return fit * 148;
-    }();
+    static std::atomic<int> known{0};
+    int resident = known;
+    if (!resident) {
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, KERNEL, kThreads, 0);
+        if (e != cudaSuccess) return e;
+        known = resident *= 148;
+    }
     const int64_t groups = (int64_t(p.out) * (p.gated ? 2 : 1) + group - 1) / group;
     const int64_t times = (p.rows + rows - 1) / rows;
-    auto blocks = [&](int slices) { return (groups * slices + kWarps - 1) / kWarps * times; };
+    auto blocks = [=](int slices) { return (groups * slices + kWarps - 1) / kWarps * times; };
     p.slices = 1;
     while (p.slices < kWarps && blocks(2 * p.slices) <= resident && p.in > step * p.slices) p.slices *= 2;
     const int64_t count = (groups + kWarps / p.slices - 1) / (kWarps / p.slices);
     if (count * times > INT32_MAX) return cudaErrorInvalidConfiguration;
     p.across = int(count);
-    return launch(kernel, dim3(unsigned(count * times)), kThreads, 0, 1, stream, p);      // in one dimension: the others end at 65535 blocks
+    return launch(KERNEL, dim3(unsigned(count * times)), kThreads, 0, 1, stream, p);      // in one dimension: the others end at 65535 blocks
 }
 
 template <typename T, bool VEC, int R> cudaError_t launch_forward(const RowsForward &p, cudaStream_t stream)
 {
-    if (p.gated) return launch_slices(rows_forward_kernel<T, VEC, R, true>, p, R, kWarpRows, 256, stream);
-    return launch_slices(rows_forward_kernel<T, VEC, R, false>, p, R, kWarpRows, 256, stream);
+    if (p.gated) return launch_slices<rows_forward_kernel<T, VEC, R, true>>(p, R, kWarpRows, 256, stream);
+    return launch_slices<rows_forward_kernel<T, VEC, R, false>>(p, R, kWarpRows, 256, stream);
 }
 
 template <int LOADS> cudaError_t launch_mma(const RowsForward &p, cudaStream_t stream)
 {
-    if (p.rows <= 8) return p.gated ? launch_slices(rows_mma_kernel<1, true, LOADS>, p, 16, 16, 32 * LOADS, stream) : launch_slices(rows_mma_kernel<1, false, LOADS>, p, 16, 16, 32 * LOADS, stream);
-    return p.gated ? launch_slices(rows_mma_kernel<2, true, LOADS>, p, 16, 16, 32 * LOADS, stream) : launch_slices(rows_mma_kernel<2, false, LOADS>, p, 16, 16, 32 * LOADS, stream);
+    if (p.rows <= 8) return p.gated ? launch_slices<rows_mma_kernel<1, true, LOADS>>(p, 16, 16, 32 * LOADS, stream) : launch_slices<rows_mma_kernel<1, false, LOADS>>(p, 16, 16, 32 * LOADS, stream);
+    return p.gated ? launch_slices<rows_mma_kernel<2, true, LOADS>>(p, 16, 16, 32 * LOADS, stream) : launch_slices<rows_mma_kernel<2, false, LOADS>>(p, 16, 16, 32 * LOADS, stream);
 }
 
 template <typename T, bool VEC> cudaError_t launch_forward_rows(const RowsForward &p, cudaStream_t stream)

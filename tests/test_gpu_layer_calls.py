@@ -1,5 +1,8 @@
 """Calls of the layer operators at the ends of what their contract allows: pitches, workspaces, row counts, kernels taken."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -92,3 +95,34 @@ def test_more_rows_than_a_grid_is_high(rows, width):
     ref = R.gated_forward(x, w, w2, b, None, 3)
     for got, k in ((h, "h"), (gate, "gate"), (up, "up")):
         check(got, ref[k], k)
+
+
+BITS = """
+import hashlib, sys, torch
+from paper_2012_05396_b200 import layers as L
+g = torch.Generator(device="cuda")
+
+def call(rows, d, f, dtype, gated=False):
+    g.manual_seed(rows * 7919 + d)
+    x, w, w2 = (torch.empty(*s, device="cuda", dtype=dtype).normal_(0, 1, generator=g) for s in ((rows, d), (f, d), (f, d)))
+    y = L.ssd_gated_forward(x, w, w2)[0] if gated else L.ssd_linear_forward(x, w)[0]
+    return hashlib.sha256(y.view(torch.uint8).cpu().numpy().tobytes()).hexdigest()
+
+f32, bf16 = torch.float32, torch.bfloat16
+calls = [(1, 4096, 4096, f32), (2, 2048, 2048, f32), (4, 4096, 1000, f32), (8, 2048, 3001, f32), (8, 2049, 3000, f32), (1, 4096, 4096, bf16),
+         (4, 1001, 2003, bf16), (8, 2048, 4096, bf16), (16, 1024, 4096, bf16), (1, 2048, 2048, f32, True), (8, 2048, 2048, f32, True), (5, 2048, 2048, bf16, True)]
+first = int(sys.argv[1])
+order = calls[first:] + calls[:first]
+sums = {c: call(*c) for c in order}
+print("\\n".join(sums[c] for c in calls))
+"""
+
+
+def test_same_bits_whatever_a_process_called_before():
+    """A few-row call's bits follow from its sizes and alignment, not from which call a process made first."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    runs = [subprocess.run([sys.executable, "-c", BITS, str(first)], cwd=root, capture_output=True, text=True, timeout=600) for first in (0, 3, 6, 8)]
+    assert all(r.returncode == 0 for r in runs), [r.stderr[-500:] for r in runs]
+    lines = [r.stdout.split() for r in runs]
+    assert len(lines[0]) == 12
+    assert all(other == lines[0] for other in lines[1:]), [[i for i, (a, b) in enumerate(zip(lines[0], o)) if a != b] for o in lines]
