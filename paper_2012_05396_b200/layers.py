@@ -171,7 +171,7 @@ class GradList:
     def __init__(self, grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None,
                  groups: Optional[Sequence[int]] = None, num_groups: Optional[int] = None, stream=None):
         where = "ssd_grad_list_create"
-        self._h = C.c_void_p()
+        self._h, self.address = C.c_void_p(), 0
         grads = list(grads)
         out = grads if out is None else list(out)
         groups = None if groups is None else [int(g) for g in groups]
@@ -200,7 +200,7 @@ class GradList:
     def ssd_grad_list_destroy(self):
         if self._h:
             lib().ssd_grad_list_destroy(self._h)
-            self._h = C.c_void_p()
+            self._h, self.address = C.c_void_p(), 0          # calls with the list are refused from here on
 
     def __del__(self):
         try:

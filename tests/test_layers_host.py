@@ -1,0 +1,25 @@
+"""Host side of the torch interface of the layer operators, with a stand-in for the library: no GPU."""
+import ctypes as C
+
+from paper_2012_05396_b200 import layers as L
+
+
+class FakeLib:
+    def __init__(self):
+        self.destroyed = []
+
+    def ssd_grad_list_destroy(self, handle):
+        self.destroyed.append(handle.value)
+
+
+def test_a_destroyed_list_has_no_address(monkeypatch):
+    """Calls pass `address` on; after the list is gone there is none, which the entry points refuse, and it is not freed twice."""
+    fake = FakeLib()
+    monkeypatch.setattr(L, "lib", lambda: fake)
+    lst = L.GradList.__new__(L.GradList)
+    lst._h, lst.address = C.c_void_p(0x1230), 0x1230
+    lst.ssd_grad_list_destroy()
+    assert fake.destroyed == [0x1230] and lst.address == 0
+    lst.ssd_grad_list_destroy()
+    del lst
+    assert fake.destroyed == [0x1230]
