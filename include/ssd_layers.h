@@ -142,8 +142,10 @@ ssd_status ssd_gated_backward(const ssd_gated_bwd *args, void *workspace, int64_
  * clips in place (the types being equal); other overlaps are not allowed (SSD_ERR_ARG).  The arrays are copied.
  * `device_table`: caller-owned device memory of ssd_grad_list_bytes() bytes, 16-byte aligned, that the
  * kernels use for as long as the list lives; ssd_grad_list_create fills it by a copy on `cuda_stream` out of
- * the list's own (pageable) memory.  Calls on one list must not overlap on the GPU: they share the table's
- * space for partial sums. */
+ * the list's own (pageable) memory and waits for that copy, so that calls may follow on any stream.  (While the
+ * stream is captured it does not wait: the copy is then part of the graph, and so are all calls on the list.)
+ * Calls on one list must not overlap on the GPU: they share the table's space for partial sums.  The list and its
+ * table outlive the calls on it, and the graphs that hold such calls. */
 typedef struct ssd_grad_list ssd_grad_list;
 ssd_status ssd_grad_list_bytes(int32_t num_tensors, const int64_t *numel, int32_t num_groups, int64_t *bytes);
 ssd_status ssd_grad_list_create(ssd_grad_list **out, int32_t num_tensors, const int64_t *numel, const int32_t *group,

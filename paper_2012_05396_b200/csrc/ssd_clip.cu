@@ -315,8 +315,13 @@ try {
     }
     while (g_at < groups) first[++g_at] = n;
     for (int32_t g = 0; g < groups; ++g) l->has_empty_group = l->has_empty_group || first[g] == first[g + 1];
-    const cudaError_t e = cudaMemcpyAsync(l->table, l->image.data(), l->image.size(), cudaMemcpyHostToDevice,
-                                          static_cast<cudaStream_t>(cuda_stream));
+    // The table holds addresses that kernels read and write by, so it is in place before the list is handed out: calls may come on any stream, and
+    // their kernels read it before they wait for their predecessors.  A copy that is captured runs with its graph.
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    cudaError_t e = cudaStreamIsCapturing(stream, &capture);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(l->table, l->image.data(), l->image.size(), cudaMemcpyHostToDevice, stream);
+    if (e == cudaSuccess && capture == cudaStreamCaptureStatusNone) e = cudaStreamSynchronize(stream);
     if (e != cudaSuccess) {
         delete l;
         return layer_cuda_fail(e);

@@ -13,6 +13,7 @@ torch.nn.Linear has them.  The last dimension is contiguous, rows may be strided
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 from typing import Optional, Sequence
 
@@ -189,12 +190,16 @@ class GradList:
         numel = (C.c_int64 * T)(*[t.numel() for t in grads])
         need = C.c_int64()
         _check(lib().ssd_grad_list_bytes(T, numel, self.num_groups, C.byref(need)), "ssd_grad_list_bytes")
-        self._keep = (grads, out, torch.empty(need.value, dtype=torch.uint8, device=self.device))
-        _check(lib().ssd_grad_list_create(
-            C.byref(self._h), T, numel, None if groups is None else (C.c_int32 * T)(*groups), self.num_groups,
-            (C.c_void_p * T)(*[t.data_ptr() for t in grads]), _DTYPES[grads[0].dtype],
-            (C.c_void_p * T)(*[t.data_ptr() for t in out]), _DTYPES[out[0].dtype],
-            self._keep[2].data_ptr(), need.value, B._stream(stream)), where)
+        # the table's memory comes from the stream that fills it, so that nothing still under way elsewhere has it
+        with torch.cuda.device(self.device), contextlib.nullcontext() if stream is None else _on(stream):
+            if torch.cuda.current_device() != self.device.index:
+                _fail(where, "the stream belongs to another device")
+            self._keep = (grads, out, torch.empty(need.value, dtype=torch.uint8, device=self.device))
+            _check(lib().ssd_grad_list_create(
+                C.byref(self._h), T, numel, None if groups is None else (C.c_int32 * T)(*groups), self.num_groups,
+                (C.c_void_p * T)(*[t.data_ptr() for t in grads]), _DTYPES[grads[0].dtype],
+                (C.c_void_p * T)(*[t.data_ptr() for t in out]), _DTYPES[out[0].dtype],
+                self._keep[2].data_ptr(), need.value, torch.cuda.current_stream().cuda_stream), where)
         self.address = self._h.value
 
     def ssd_grad_list_destroy(self):
