@@ -4,6 +4,7 @@
 #include "ssd_layers.h"
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -331,11 +332,11 @@ PyObject *gated_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (list address, device index, groups, max_norm or None for the norms alone, nonfinite, norms)
+// (list address, device index, groups, max_norm or None for the norms alone, nonfinite, norms, table, the stream that the table is memory of)
 PyObject *clip(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    const bool scale = n == 6 && a[3] != Py_None;
-    return guarded(scale ? "ssd_clip_grad_norm" : "ssd_grad_norm", n, 6, [&]() -> PyObject * {
+    const bool scale = n == 8 && a[3] != Py_None;
+    return guarded(scale ? "ssd_clip_grad_norm" : "ssd_grad_norm", n, 8, [&]() -> PyObject * {
         ssd_grad_list *list = static_cast<ssd_grad_list *>(PyLong_AsVoidPtr(a[0]));
         const c10::Device device(c10::kCUDA, c10::DeviceIndex(as_int(a[1])));
         const int64_t groups = as_int(a[2]);
@@ -349,7 +350,13 @@ PyObject *clip(PyObject *, PyObject *const *a, Py_ssize_t n)
             if (norms.scalar_type() != at::kFloat || norms.device() != device || norms.numel() != groups || !norms.is_contiguous())
                 throw Fail{SSD_ERR_ARG, "norms is not a contiguous float32 tensor with one value per group on the gradients' device"};
         }
-        void *stream = c10::cuda::getCurrentCUDAStream(device.index()).stream();
+        const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(device.index());
+        void *stream = current.stream();
+        // on another stream than its own, the table's memory stays taken until this call is done there
+        if (stream != PyLong_AsVoidPtr(a[7]) && list) {
+            if (!THPVariable_Check(a[6])) throw Fail{SSD_ERR_ARG, "the list has no table"};
+            c10::cuda::CUDACachingAllocator::recordStream(THPVariable_Unpack(a[6]).storage().data_ptr(), current);
+        }
         float *out = static_cast<float *>(norms.data_ptr());
         if (scale) {
             const double limit = PyFloat_AsDouble(a[3]);

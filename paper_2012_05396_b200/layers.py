@@ -194,12 +194,13 @@ class GradList:
         with torch.cuda.device(self.device), contextlib.nullcontext() if stream is None else _on(stream):
             if torch.cuda.current_device() != self.device.index:
                 _fail(where, "the stream belongs to another device")
-            self._keep = (grads, out, torch.empty(need.value, dtype=torch.uint8, device=self.device))
+            self._keep = (grads, out)
+            self.table, self.home = torch.empty(need.value, dtype=torch.uint8, device=self.device), torch.cuda.current_stream().cuda_stream
             _check(lib().ssd_grad_list_create(
                 C.byref(self._h), T, numel, None if groups is None else (C.c_int32 * T)(*groups), self.num_groups,
                 (C.c_void_p * T)(*[t.data_ptr() for t in grads]), _DTYPES[grads[0].dtype],
                 (C.c_void_p * T)(*[t.data_ptr() for t in out]), _DTYPES[out[0].dtype],
-                self._keep[2].data_ptr(), need.value, torch.cuda.current_stream().cuda_stream), where)
+                self.table.data_ptr(), need.value, self.home), where)
         self.address = self._h.value
 
     def ssd_grad_list_destroy(self):
@@ -219,7 +220,7 @@ def ssd_clip_grad_norm(grads: GradList, max_norm: float, nonfinite: int = SSD_NO
     if stream is not None:
         with _on(stream):
             return ssd_clip_grad_norm(grads, max_norm, nonfinite, norms)
-    return (_torch or _marshal()).clip(grads.address, grads.device.index, grads.num_groups, max_norm, nonfinite, norms)
+    return (_torch or _marshal()).clip(grads.address, grads.device.index, grads.num_groups, max_norm, nonfinite, norms, grads.table, grads.home)
 
 
 def ssd_grad_norm(grads: GradList, norms=None, stream=None):
@@ -227,7 +228,7 @@ def ssd_grad_norm(grads: GradList, norms=None, stream=None):
     if stream is not None:
         with _on(stream):
             return ssd_grad_norm(grads, norms)
-    return (_torch or _marshal()).clip(grads.address, grads.device.index, grads.num_groups, None, 0, norms)
+    return (_torch or _marshal()).clip(grads.address, grads.device.index, grads.num_groups, None, 0, norms, grads.table, grads.home)
 
 
 def ssd_layer_error() -> int:

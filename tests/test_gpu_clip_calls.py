@@ -39,8 +39,53 @@ def test_the_table_is_memory_of_the_stream_that_fills_it(raw):
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     lst = L.GradList(g, groups=[0, 1], stream=side.cuda_stream if raw else side)
-    assert allocated_on(lst._keep[2]) == side.cuda_stream
-    assert allocated_on(L.GradList(g)._keep[2]) == torch.cuda.current_stream().cuda_stream
+    assert allocated_on(lst.table) == side.cuda_stream
+    assert allocated_on(L.GradList(g).table) == torch.cuda.current_stream().cuda_stream
     # the table is in place when the list is: a call on any stream may follow
     norms = L.ssd_grad_norm(lst)
     assert torch.allclose(norms, torch.tensor([3.0 * 5000 ** 0.5, 4.0 * 700 ** 0.5], device="cuda"), rtol=1e-6)
+
+
+def test_a_list_dropped_while_another_stream_uses_it():
+    """The table's memory is not handed out again before the calls on it are done, whichever stream they run on."""
+    n = 300000
+    g = torch.full((n,), 2.0, device="cuda")
+    norms = torch.empty(1, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    lst = L.GradList([g])
+    at, size = lst.table.data_ptr(), lst.table.numel()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)              # a tenth of a second
+    L.ssd_clip_grad_norm(lst, 1.0, norms=norms, stream=side)
+    del lst
+    assert not side.query()
+    fresh = [torch.full((size,), 255, device="cuda", dtype=torch.uint8) for _ in range(8)]
+    assert all(not (t.data_ptr() <= at < t.data_ptr() + size) for t in fresh)
+    side.synchronize()
+    assert abs(float(norms) - 2.0 * n ** 0.5) <= 1e-3
+    assert torch.allclose(g, torch.full_like(g, n ** -0.5), rtol=1e-5)
+
+
+def test_captured_into_a_graph():
+    """A call captured on another stream than the list's, replayed on new gradients, and the list dropped afterwards."""
+    g = torch.empty(40000, device="cuda")
+    out = torch.empty(40000, device="cuda", dtype=torch.bfloat16)
+    norms = torch.empty(2, device="cuda")
+    lst = L.GradList([g[:30000], g[30000:]], out=[out[:30000], out[30000:]], groups=[0, 1])
+    g.fill_(1.0)
+    L.ssd_clip_grad_norm(lst, 2.0, norms=norms)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.ssd_clip_grad_norm(lst, 2.0, norms=norms)
+    for v in (0.5, 8.0, 1e-3):
+        g.fill_(v)
+        graph.replay()
+        want = torch.tensor([v * 30000 ** 0.5, v * 10000 ** 0.5], device="cuda")
+        assert torch.allclose(norms, want, rtol=1e-6)
+        for part, n in ((out[:30000], want[0]), (out[30000:], want[1])):
+            f = min(1.0, 2.0 / (float(n) + 1e-6))
+            assert torch.allclose(part.float(), torch.full_like(part, v * f, dtype=torch.float32), rtol=2.0 ** -8, atol=0)
+    torch.cuda.synchronize()
+    del graph, lst
+    assert float(L.ssd_grad_norm(L.GradList([g]))) > 0

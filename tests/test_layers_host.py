@@ -23,3 +23,24 @@ def test_a_destroyed_list_has_no_address(monkeypatch):
     lst.ssd_grad_list_destroy()
     del lst
     assert fake.destroyed == [0x1230]
+
+
+class FakeMarshal:
+    def __init__(self):
+        self.calls = []
+
+    def clip(self, *args):
+        self.calls.append(args)
+
+
+def test_calls_name_the_table_and_its_stream(monkeypatch):
+    """What ties the table's memory to the stream of a call (it may be another than the table's own) needs both."""
+    fake = FakeMarshal()
+    monkeypatch.setattr(L, "_torch", fake)
+    monkeypatch.setattr(L, "lib", lambda: FakeLib())
+    lst = L.GradList.__new__(L.GradList)
+    lst._h, lst.address, lst.num_groups, lst.device = C.c_void_p(0), 0x1230, 3, type("D", (), {"index": 0})
+    lst.table, lst.home = object(), 0x770
+    L.ssd_clip_grad_norm(lst, 1.5)
+    L.ssd_grad_norm(lst)
+    assert fake.calls == [(0x1230, 0, 3, 1.5, 0, None, lst.table, 0x770), (0x1230, 0, 3, None, 0, None, lst.table, 0x770)]
