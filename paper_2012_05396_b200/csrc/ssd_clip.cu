@@ -6,9 +6,8 @@
 // (read + read + write; the second read comes out of the 126 MB L2 as far as it fits).  The tensors are
 // cut into chunks of one thread block each, listed in a device table, so that 1 tensor of 10^9 elements and
 // 6000 small ones make the same kind of launch.
-// Measured: 8 arenas of 25.6 M float32 into bfloat16 318 us (reading twice and writing once at the copy rate is 312); 16 of 138 M
-// bfloat16 2.07 ms (2.03); 4 of 0.27 M 7.0 us, two launches whose start overlaps (9.4 when the second loaded nothing before the first
-// was done).
+// Measured: 8 arenas of 25.6 M float32 into bfloat16 313 us (reading twice and writing once at the copy rate is 312); 16 of 138 M
+// bfloat16 2.07 ms (2.03); 4 of 0.27 M 7.1 us, two launches whose start overlaps, in place with nothing to scale 6.0, the norms alone 4.2.
 #include "ssd_layers.h"
 #include "ssd_layers_common.cuh"
 
@@ -87,7 +86,16 @@ struct ClipParams {
     float max_norm;
     int32_t zero_nonfinite;
     int32_t num_chunks;
+    int32_t captured;             // the table's copy is part of a graph, as this kernel is
 };
+
+// A block's share.  The table is in place before the list is handed out, so it is read while the kernel before this one still runs; gradients and
+// whatever else kernels write are read after wait_for_previous only, which is what makes their stores visible.
+__device__ __forceinline__ Chunk chunk_at(const ClipParams &p, unsigned i)
+{
+    if (p.captured) wait_for_previous();
+    return p.chunks[i];
+}
 
 template <typename T> __device__ __forceinline__ float widen(T v);
 template <> __device__ __forceinline__ float widen<float>(float v) { return v; }
@@ -116,9 +124,9 @@ __device__ __forceinline__ double block_sum(double v)
 template <typename T> __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ ClipParams p)
 {
     constexpr int V = 16 / sizeof(T);
-    const Chunk c = p.chunks[blockIdx.x];       // the table is as old as the list
+    const Chunk c = chunk_at(p, blockIdx.x);
     wait_for_previous();
-    dependents_may_start();                     // only now: scale_kernel reads gradients before it waits
+    dependents_may_start();                     // not before: scale_kernel's blocks, come up this early, would only be in the way (4 x ResNet-20: 8.9 us for 7.1)
     const T *g = reinterpret_cast<const T *>(c.src);
     // elements before the first 16-byte boundary, whole vectors, rest
     int head = int(((16 - (c.src & 15)) & 15) / sizeof(T));
@@ -179,7 +187,7 @@ template <typename S, typename D> __global__ void __launch_bounds__(kThreads) sc
 {
     constexpr int V = 16 / (sizeof(S) > sizeof(D) ? sizeof(S) : sizeof(D));
     dependents_may_start();
-    const Chunk c = p.chunks[p.num_chunks - 1 - blockIdx.x];
+    const Chunk c = chunk_at(p, p.num_chunks - 1 - blockIdx.x);
     const S *g = reinterpret_cast<const S *>(c.src);
     D *o = reinterpret_cast<D *>(c.dst);
     // vectors where source and destination reach a vector boundary at the same element
@@ -190,8 +198,6 @@ template <typename S, typename D> __global__ void __launch_bounds__(kThreads) sc
     else head = 0;
     const Pack<S, V> *gv = reinterpret_cast<const Pack<S, V> *>(g + head);
     Pack<D, V> *ov = reinterpret_cast<Pack<D, V> *>(o + head);
-    // The gradients are what norm_kernel, which has started, waited for, and nothing writes them since: the first of them are loaded while
-    // it is still adding up.
     constexpr int kAtOnce = 4;
     Pack<S, V> x[kAtOnce];
     auto fetch = [&](int i) {
@@ -199,8 +205,8 @@ template <typename S, typename D> __global__ void __launch_bounds__(kThreads) sc
         for (int q = 0; q < kAtOnce; ++q)
             if (i + q * kThreads < nvec) x[q] = gv[i + q * kThreads];
     };
-    fetch(threadIdx.x);
     wait_for_previous();
+    fetch(threadIdx.x);                         // on their way together with the factor
     const float f = __ldcg(&p.factor[c.group]);
     if (f == 1.0f && c.src == c.dst) return;
     const bool zero = f == 0.0f && p.zero_nonfinite;      // nothing of an infinity or NaN may stay
@@ -228,6 +234,7 @@ struct ssd_grad_list {
     int32_t src_dtype = 0, dst_dtype = 0;
     bool has_empty_group = false;
     bool writes = false;              // some destination is not its source
+    bool captured = false;            // created while its stream was captured
     TableLayout at{};
     unsigned char *table = nullptr;   // the caller's device memory
     std::vector<unsigned char> image;
@@ -316,12 +323,13 @@ try {
     while (g_at < groups) first[++g_at] = n;
     for (int32_t g = 0; g < groups; ++g) l->has_empty_group = l->has_empty_group || first[g] == first[g + 1];
     // The table holds addresses that kernels read and write by, so it is in place before the list is handed out: calls may come on any stream, and
-    // their kernels read it before they wait for their predecessors.  A copy that is captured runs with its graph.
+    // their kernels read it before they wait for their predecessors (not where the copy is captured: it then runs with its graph).
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
     cudaError_t e = cudaStreamIsCapturing(stream, &capture);
     if (e == cudaSuccess) e = cudaMemcpyAsync(l->table, l->image.data(), l->image.size(), cudaMemcpyHostToDevice, stream);
-    if (e == cudaSuccess && capture == cudaStreamCaptureStatusNone) e = cudaStreamSynchronize(stream);
+    l->captured = capture != cudaStreamCaptureStatusNone;
+    if (e == cudaSuccess && !l->captured) e = cudaStreamSynchronize(stream);
     if (e != cudaSuccess) {
         delete l;
         return layer_cuda_fail(e);
@@ -350,6 +358,7 @@ static ssd_status clip_call(ssd_grad_list *l, float max_norm, int32_t nonfinite,
     p.max_norm = max_norm;
     p.zero_nonfinite = nonfinite == SSD_NONFINITE_ZERO;
     p.num_chunks = l->chunks;
+    p.captured = l->captured;
     cudaError_t e = cudaSuccess;
     auto run = [&](auto kernel, int blocks, auto... args) {
         if (e != cudaSuccess) return;

@@ -89,3 +89,29 @@ def test_captured_into_a_graph():
     torch.cuda.synchronize()
     del graph, lst
     assert float(L.ssd_grad_norm(L.GradList([g]))) > 0
+
+
+@pytest.mark.parametrize("sizes", [[5000] * 40, [3_000_000, 17, 40_000]], ids=["small", "large"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_gradients_written_by_the_kernel_before(sizes, in_place):
+    """Every call sees what the kernel directly before it wrote, none of the values of the call before."""
+    total = sum(sizes)
+    arena, other = torch.empty(total, device="cuda"), torch.empty(total, device="cuda")
+    views, at = [], 0
+    for n in sizes:
+        views.append((arena[at:at + n], other[at:at + n]))
+        at += n
+    lst = L.GradList([a for a, _ in views], out=None if in_place else [b for _, b in views])
+    base = torch.randn(total, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5))
+    unit = base / float(base.double().norm())
+    out = arena if in_place else other
+    seen = []
+    for i in range(200):
+        torch.mul(base, float(1 + i % 7), out=arena)
+        norm = L.ssd_clip_grad_norm(lst, 1.0)
+        seen.append((norm, (out - unit).abs().max()))
+    norms = torch.stack([n[0] for n, _ in seen]).double()
+    want = float(base.double().norm()) * torch.tensor([1.0 + i % 7 for i in range(200)], dtype=torch.float64, device="cuda")
+    # the products base * i and the factor round to float32 (2^-24 each); 1e-6 is added to norms of 400 and more
+    assert bool(((norms - want).abs() <= 2.0 ** -21 * want).all())
+    assert float(torch.stack([d for _, d in seen]).max()) <= 2.0 ** -20 * float(unit.abs().max())
