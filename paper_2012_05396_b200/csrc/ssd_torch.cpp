@@ -161,14 +161,14 @@ template <typename... T> PyObject *pack(const T &...t)
     return nullptr;
 }
 
-long as_int(PyObject *o)
+int32_t as_int(PyObject *o)
 {
     const long v = PyLong_AsLong(o);
-    if (v == -1 && PyErr_Occurred()) {
+    if ((v == -1 && PyErr_Occurred()) || v != int32_t(v)) {
         PyErr_Clear();
-        throw Fail{SSD_ERR_ARG, "an integer is expected"};
+        throw Fail{SSD_ERR_ARG, "an integer of 32 bits is expected"};
     }
-    return v;
+    return int32_t(v);
 }
 
 template <typename F> PyObject *guarded(const char *where, Py_ssize_t n, Py_ssize_t expected, F f)
@@ -189,7 +189,7 @@ template <typename F> PyObject *guarded(const char *where, Py_ssize_t n, Py_ssiz
 }
 
 // The weight gradients' type: that of the first tensor given for one, else the code (-1: float32).
-at::ScalarType grad_type(const Call &c, std::initializer_list<PyObject *> given, long code)
+at::ScalarType grad_type(const Call &c, std::initializer_list<PyObject *> given, int32_t code)
 {
     for (PyObject *o : given)
         if (o != Py_None) {
@@ -209,7 +209,7 @@ PyObject *linear_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const Mat x = c.flat(a[0], -1, -1, "x"), w = c.flat(a[1], x.cols, -1, "weight");
         const auto shape = shape_like(tx, w.rows);
         const at::Tensor y = c.output(a[2], true, shape, "y", c.dtype), z = c.output(a[5], a[7] == Py_True, shape, "z", c.dtype);
-        ssd_linear_fwd s{x.rows, x.cols, w.rows, c.code(), int32_t(as_int(a[6])), x.p, x.ld, w.p, w.ld};
+        ssd_linear_fwd s{x.rows, x.cols, w.rows, c.code(), as_int(a[6]), x.p, x.ld, w.p, w.ld};
         s.bias = static_cast<const float *>(c.vector(a[3], w.rows, "bias", at::kFloat));
         if (a[4] != Py_None) {
             const Mat r = c.flat(a[4], w.rows, x.rows, "residual");
@@ -238,7 +238,7 @@ PyObject *linear_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const at::ScalarType g = grad_type(c, {a[6], a[7]}, as_int(a[8]));
         const at::Tensor dx = c.output(a[5], a[9] == Py_True, THPVariable_Unpack(a[1]).sizes(), "dx", c.dtype);
         const at::Tensor dw = c.output(a[6], a[10] == Py_True, {dy.cols, w.cols}, "dweight", g), db = c.output(a[7], a[11] == Py_True, {dy.cols}, "dbias", g);
-        ssd_linear_bwd s{dy.rows, w.cols, dy.cols, c.code(), int32_t(as_int(a[4])), Call::code_of(g), 0, dy.p, dy.ld, x.p, x.ld, w.p, w.ld};
+        ssd_linear_bwd s{dy.rows, w.cols, dy.cols, c.code(), as_int(a[4]), Call::code_of(g), 0, dy.p, dy.ld, x.p, x.ld, w.p, w.ld};
         if (a[3] != Py_None) {
             const Mat z = c.flat(a[3], dy.cols, dy.rows, "z");
             s.z = z.p;
@@ -273,7 +273,7 @@ PyObject *gated_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const auto shape = shape_like(tx, g.rows);
         const bool keep = a[9] == Py_True;
         const at::Tensor h = c.output(a[5], true, shape, "h", c.dtype), gate = c.output(a[6], keep, shape, "gate", c.dtype), up = c.output(a[7], keep, shape, "up", c.dtype);
-        ssd_gated_fwd s{x.rows, x.cols, g.rows, c.code(), int32_t(as_int(a[8])), x.p, x.ld, g.p, g.ld, u.p, u.ld};
+        ssd_gated_fwd s{x.rows, x.cols, g.rows, c.code(), as_int(a[8]), x.p, x.ld, g.p, g.ld, u.p, u.ld};
         s.b_gate = static_cast<const float *>(c.vector(a[3], g.rows, "b_gate", at::kFloat));
         s.b_up = static_cast<const float *>(c.vector(a[4], g.rows, "b_up", at::kFloat));
         const Mat mh = c.flat(h, g.rows, x.rows, "h", c.dtype);
@@ -306,7 +306,7 @@ PyObject *gated_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const at::Tensor dx = c.output(a[7], a[13] == Py_True, THPVariable_Unpack(a[1]).sizes(), "dx", c.dtype);
         const at::Tensor dwg = c.output(a[8], want_dw, {dh.cols, wg.cols}, "dw_gate", g), dwu = c.output(a[9], want_dw, {dh.cols, wg.cols}, "dw_up", g);
         const at::Tensor dbg = c.output(a[10], want_db, {dh.cols}, "db_gate", g), dbu = c.output(a[11], want_db, {dh.cols}, "db_up", g);
-        ssd_gated_bwd s{dh.rows, wg.cols, dh.cols, c.code(), int32_t(as_int(a[6])), Call::code_of(g), 0, dh.p, dh.ld, x.p, x.ld,
+        ssd_gated_bwd s{dh.rows, wg.cols, dh.cols, c.code(), as_int(a[6]), Call::code_of(g), 0, dh.p, dh.ld, x.p, x.ld,
                         wg.p, wg.ld, wu.p, wu.ld, gate.p, gate.ld, up.p, up.ld};
         if (dx.defined()) {
             const Mat m = c.flat(dx, wg.cols, dh.rows, "dx", c.dtype);
@@ -364,7 +364,7 @@ PyObject *clip(PyObject *, PyObject *const *a, Py_ssize_t n)
                 PyErr_Clear();
                 throw Fail{SSD_ERR_ARG, "max_norm is not a number"};
             }
-            Call::check(g_clip(list, float(limit), int32_t(as_int(a[4])), out, stream));
+            Call::check(g_clip(list, float(limit), as_int(a[4]), out, stream));
         } else {
             Call::check(g_norm(list, out, stream));
         }

@@ -182,6 +182,8 @@ class GradList:
         for ts in (grads, out):
             if any(t.dtype != ts[0].dtype or t.device != self.device or not t.is_contiguous() for t in ts):
                 _fail(where, "tensors are contiguous, on one device and of one type")
+        if not -1 << 31 <= self.num_groups < 1 << 31 or (groups is not None and not all(-1 << 31 <= g < 1 << 31 for g in groups)):
+            _fail(where, "group numbers are integers of 32 bits")
         if any(a.numel() != b.numel() for a, b in zip(grads, out)):
             _fail(where, "a destination has another size")
         if not grads[0].is_cuda or grads[0].dtype not in _DTYPES or out[0].dtype not in _DTYPES:

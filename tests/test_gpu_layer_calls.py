@@ -126,3 +126,20 @@ def test_same_bits_whatever_a_process_called_before():
     lines = [r.stdout.split() for r in runs]
     assert len(lines[0]) == 12
     assert all(other == lines[0] for other in lines[1:]), [[i for i, (a, b) in enumerate(zip(lines[0], o)) if a != b] for o in lines]
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    """They do not wrap around into a valid one."""
+    g = gen(6)
+    x, w = normal(g, 4, 8, dtype=torch.float32), normal(g, 6, 8, dtype=torch.float32)
+    y, z = L.ssd_linear_forward(x, w, act=2, keep=True)
+    a = torch.zeros(64, device="cuda")
+    lst = L.GradList([a])
+    calls = [lambda v: L.ssd_linear_forward(x, w, act=v), lambda v: L.ssd_gated_forward(x, w, w.clone(), act=v), lambda v: L.ssd_linear_backward(y, x, w, z, act=v),
+             lambda v: L.ssd_gated_backward(y, x, w, w.clone(), z, z.clone(), act=v), lambda v: L.ssd_clip_grad_norm(lst, 1.0, nonfinite=v),
+             lambda v: L.GradList([a], groups=[v]), lambda v: L.GradList([a], num_groups=v)]
+    for call in calls:
+        for v in (1 << 32, (1 << 32) + 1, -(1 << 32), 1 << 63, 1 << 70):
+            with pytest.raises(B.SsdError) as e:
+                call(v)
+            assert e.value.status == B.SSD_ERR_ARG
