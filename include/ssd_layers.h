@@ -157,7 +157,7 @@ void ssd_grad_list_destroy(ssd_grad_list *list);
  * so that the update sees nothing of it.  The norm reports it either way. */
 typedef enum { SSD_NONFINITE_KEEP = 0, SSD_NONFINITE_ZERO = 1 } ssd_nonfinite;
 
-/* norms: device array of num_groups floats.  max_norm >= 0, or +infinity for no limit (dst is then a copy of src, or
+/* norms: device array of num_groups floats, apart from gradients, destinations and table (SSD_ERR_ARG).  max_norm >= 0, or +infinity for no limit (dst is then a copy of src, or
  * left alone in place).  A group that needs no scaling is not written when in place. */
 ssd_status ssd_clip_grad_norm(ssd_grad_list *list, float max_norm, int32_t nonfinite, float *norms, void *cuda_stream);
 

@@ -15,7 +15,10 @@
 
 #include <cmath>
 #include <cstring>
+#include <iterator>
+#include <memory>
 #include <new>
+#include <utility>
 #include <vector>
 
 namespace {
@@ -238,6 +241,7 @@ struct ssd_grad_list {
     TableLayout at{};
     unsigned char *table = nullptr;   // the caller's device memory
     std::vector<unsigned char> image;
+    std::vector<std::pair<uintptr_t, uintptr_t>> taken;      // address ranges of gradients, destinations and table: ascending, apart from each other
 };
 
 extern "C" {
@@ -297,7 +301,8 @@ try {
         else read = s.hi > read ? s.hi : read;
     }
 
-    ssd_grad_list *l = new ssd_grad_list;
+    std::unique_ptr<ssd_grad_list> owned(new ssd_grad_list);       // until it is handed out
+    ssd_grad_list *const l = owned.get();
     l->groups = groups;
     l->chunks = int32_t(nchunks);
     l->src_dtype = src_dtype;
@@ -306,6 +311,10 @@ try {
     l->at = at;
     l->table = static_cast<unsigned char *>(device_table);
     l->image.assign(size_t(at.bytes), 0);
+    for (const Span &s : spans) {
+        if (l->taken.empty() || s.lo > l->taken.back().second) l->taken.emplace_back(s.lo, s.hi);
+        else l->taken.back().second = std::max(l->taken.back().second, s.hi);
+    }
     Chunk *c = reinterpret_cast<Chunk *>(l->image.data() + at.chunks);
     int32_t *first = reinterpret_cast<int32_t *>(l->image.data() + at.group_first);
     int32_t n = 0, g_at = 0;
@@ -330,11 +339,8 @@ try {
     if (e == cudaSuccess) e = cudaMemcpyAsync(l->table, l->image.data(), l->image.size(), cudaMemcpyHostToDevice, stream);
     l->captured = capture != cudaStreamCaptureStatusNone;
     if (e == cudaSuccess && !l->captured) e = cudaStreamSynchronize(stream);
-    if (e != cudaSuccess) {
-        delete l;
-        return layer_cuda_fail(e);
-    }
-    *out = l;
+    if (e != cudaSuccess) return layer_cuda_fail(e);
+    *out = owned.release();
     return SSD_OK;
 } catch (const std::bad_alloc &) {
     return SSD_ERR_NOMEM;
@@ -347,6 +353,10 @@ static ssd_status clip_call(ssd_grad_list *l, float max_norm, int32_t nonfinite,
     if (!l || !norms || !(max_norm >= 0.0f)) return SSD_ERR_ARG;
     if (nonfinite != SSD_NONFINITE_KEEP && nonfinite != SSD_NONFINITE_ZERO) return SSD_ERR_ARG;
     if (reinterpret_cast<uintptr_t>(norms) & 3) return SSD_ERR_ALIGN;
+    // the norms lie over nothing that the call reads or writes: the last range that starts before their end ends before them
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(norms), hi = lo + uintptr_t(l->groups) * 4;
+    const auto after = std::partition_point(l->taken.begin(), l->taken.end(), [&](const auto &range) { return range.first < hi; });
+    if (after != l->taken.begin() && std::prev(after)->second > lo) return SSD_ERR_ARG;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     ClipParams p{};
     p.chunks = reinterpret_cast<const Chunk *>(l->table + l->at.chunks);
