@@ -14,7 +14,8 @@
 
 namespace {
 
-PyObject *g_error = nullptr;      // SsdError(status, where, detail)
+PyObject *g_error = nullptr;             // SsdError(status, where, detail)
+PyObject *g_memory_error = nullptr;      // torch.OutOfMemoryError
 
 struct Entry {
     ssd_status (*workspace)(const void *, int64_t *);
@@ -182,7 +183,9 @@ template <typename F> PyObject *guarded(const char *where, Py_ssize_t n, Py_ssiz
             PyErr_SetObject(g_error, x);
             Py_DECREF(x);
         }
-    } catch (const std::exception &e) {      // torch's allocator: out of memory
+    } catch (const c10::OutOfMemoryError &e) {      // torch's allocator
+        PyErr_SetString(g_memory_error, e.what_without_backtrace());
+    } catch (const std::exception &e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
     }
     return nullptr;
@@ -372,11 +375,11 @@ PyObject *clip(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (SsdError, {entry point: address})
+// (SsdError, {entry point: address}, torch.OutOfMemoryError)
 PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (n != 2 || !PyDict_Check(a[1])) {
-        PyErr_SetString(PyExc_TypeError, "setup(error class, {name: address})");
+    if (n != 3 || !PyDict_Check(a[1])) {
+        PyErr_SetString(PyExc_TypeError, "setup(error class, {name: address}, class of the allocator's error)");
         return nullptr;
     }
     bool ok = true;
@@ -402,6 +405,9 @@ PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n)
     Py_INCREF(a[0]);
     Py_XDECREF(g_error);
     g_error = a[0];
+    Py_INCREF(a[2]);
+    Py_XDECREF(g_memory_error);
+    g_memory_error = a[2];
     Py_RETURN_NONE;
 }
 

@@ -102,7 +102,7 @@ def _marshal():
     if _torch is None:
         L = lib()
         from . import _ssd_torch
-        _ssd_torch.setup(SsdError, {name: C.cast(getattr(L, name), C.c_void_p).value for name in EXPORTS})
+        _ssd_torch.setup(SsdError, {name: C.cast(getattr(L, name), C.c_void_p).value for name in EXPORTS}, torch.OutOfMemoryError)
         _torch = _ssd_torch
     return _torch
 

@@ -143,3 +143,12 @@ def test_numbers_beyond_32_bits_are_refused():
             with pytest.raises(B.SsdError) as e:
                 call(v)
             assert e.value.status == B.SSD_ERR_ARG
+
+
+def test_running_out_of_memory_is_torchs_error():
+    """A result that no card holds (1.4 TB): what torch's own operators raise, and the next call works."""
+    x, w = torch.ones(600000, 1, device="cuda"), torch.ones(600000, 1, device="cuda")
+    with pytest.raises(torch.OutOfMemoryError):
+        L.ssd_linear_forward(x, w)
+    y, _ = L.ssd_linear_forward(x[:3], w[:5])
+    assert bool((y == 1.0).all())
