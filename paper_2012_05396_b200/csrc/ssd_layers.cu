@@ -289,18 +289,42 @@ void product(Call &c, Product &p)
 //   bfloat16 forward 4096 x 4096, 1 row 6.4 / 10, 8 rows 10.6 / 10.6, 16 rows 9.6 / 10.7; 1024 x 1024, 8 rows 2.8 / 5.2;
 //                    gated 2048 x 8192, 8 rows 14.3 / 16.1, 16 rows 16.2 / 16.3
 //                    1001 x 2003 (rows that lie anywhere), 4 rows 5.7 / 9.9, 8 rows 13 / 9.9; 301 x 200, 30 rows 6.9 / 5.9
-//   float32 forward of more rows, eight at a time: 64 x 512 x 512 4.1 / 9.5, 24 x 1024 x 1024 6.2 / 13.6 (gated 9.9 / 15.4)
+//   float32 forward of more rows, eight at a time: 64 x 512 x 512 4.4 / 9.5, 24 x 1024 x 1024 6.2 / 13.6 (gated 9.9 / 15.4), 1024 x 64 x 10 3.4 / 9.5,
+//                    7000 x 1000 x 8 24 / 30; but 1000 x 64 x 1000 38 / 9.7, 8000 x 8 x 1000 289 / 32, 250 x 500 x 500 30 / 16, 100000 x 1 x 64 240 / 99
 //   backward (float32 weight gradients) 4096 x 4096, 8 rows 36 / 54 bfloat16, 39 / 111 float32; 16 rows 51 / 54, 54 / 112;
 //                    256 x 256, 16 rows 6.7 / 16.4 bfloat16
-// so multiply-adds take float32 up to the number of weights, counted once for every eight rows, where both sides come out even, and bfloat16
-// rows that lie anywhere up to less of it.
+// so multiply-adds take float32 of up to 16 rows, and of more where both sides' estimates say so (over 300 drawn calls 0.4 % slower than the better side of
+// each, 1.4 times at worst), and bfloat16 rows that lie anywhere up to a number of weights, counted once for every eight rows.
 constexpr int kFewRowsMost = 16;
-constexpr double kFewEights = 8e6, kFewEightsAnywhere = 2.5e6;
+constexpr double kFewEightsAnywhere = 2.5e6;
+
+// Estimated time of a float32 forward on the tensor cores: the pass that brings the operands into parts (2 us for each time a warp goes
+// through its rows of them, 5 TB/s where there is much of it), and the product.
+double parts_forward_us(const Forward &f)
+{
+    Product p{};
+    p.m = int(f.rows);
+    p.n = int(f.out);
+    p.k = int(f.in);
+    p.nseg = 6;
+    p.nmain = p.groups = 1;
+    p.gated = f.mats == 2;
+    p.e = f.e;
+    p.e.vec = row_alignment(p);
+    auto turns = [&](int64_t rows) { return double((std::min<int64_t>(prep_rows_per_chunk(rows, f.in), rows) + 2 * kPrepWarps - 1) / (2 * kPrepWarps)); };
+    const double bytes = 10.0 * double(f.in) * (double(f.rows) + double(f.mats) * double(f.out));
+    return 2.0 + std::max(2.0 * std::max(turns(f.rows), turns(f.out)), bytes / 5e6) + product_us(p);
+}
+
+RowsForward rows_of(const Forward &f)
+{
+    return RowsForward{f.x, {f.w[0], f.w[1]}, f.ldx, {f.ldw[0], f.ldw[1]}, int(f.rows), int(f.in), int(f.out), f.mats == 2, 0, 0, f.e};
+}
 
 bool few_rows(const Forward &f)
 {
+    if (f.dtype == SSD_F32) return f.rows <= kFewRowsMost || rows_forward_f32_us(rows_of(f)) <= parts_forward_us(f);
     const double eights = double((f.rows + 7) / 8) * double(f.out) * double(f.in) * f.mats;      // weights read by eight rows at a time
-    if (f.dtype == SSD_F32) return f.rows <= kFewRowsMost || eights <= kFewEights;
     bool aligned = tma_can_read(f.x, f.ldx, f.rows, f.dtype) && f.in % 8 == 0;
     for (int i = 0; i < f.mats; ++i) aligned = aligned && tma_can_read(f.w[i], f.ldw[i], f.out, f.dtype);
     if (aligned) return f.rows <= kFewRowsMost;
@@ -313,9 +337,8 @@ void run_forward(Call &c, const Forward &f)
 {
     if (f.rows == 0) return;
     if (few_rows(f)) {
-        RowsForward q{f.x, {f.w[0], f.w[1]}, f.ldx, {f.ldw[0], f.ldw[1]}, int(f.rows), int(f.in), int(f.out), f.mats == 2, 0, 0, f.e};
         if (c.live()) {
-            const cudaError_t e = launch_rows_forward(q, c.stream);
+            const cudaError_t e = launch_rows_forward(rows_of(f), c.stream);
             if (c.err == cudaSuccess) c.err = e;
         }
         return;

@@ -62,6 +62,7 @@ struct Product {
 // sizes and on e.vec alone.
 int64_t product_partial_floats(const Product &p);
 cudaError_t launch_product(const Product &p, float *partial, cudaStream_t stream);
+double product_us(const Product &p);      // its estimated time: of p the sizes, groups, gated, nseg and e.vec
 
 // A few rows (csrc/ssd_rows.cu).
 
@@ -83,6 +84,7 @@ struct RowsBackward {
 };
 
 cudaError_t launch_rows_forward(RowsForward p, cudaStream_t stream);        // these count their launches themselves
+double rows_forward_f32_us(const RowsForward &p);                           // the estimated time for float32 and more than four rows
 int64_t rows_partial_floats(int rows, int out, int in);
 cudaError_t launch_rows_backward(RowsBackward p, cudaStream_t stream);
 

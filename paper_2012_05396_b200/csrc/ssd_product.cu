@@ -617,18 +617,15 @@ template <int BN, bool AMN, bool BMN, bool GATED, bool DRAIN> cudaError_t launch
 // A round is what fits the chip at a time: 74 pairs, and clusters as cudaOccupancyMaxActiveClusters gives them for tile_kernel's blocks.
 struct Choice {
     int kind, split;       // kind: columns of a pair's tile, or 0 for tile_kernel
+    double us;
 };
 
 Choice choose(const Product &p)
 {
     const double steps = double((p.k + kBlockK - 1) / kBlockK) * p.nseg;
-    Choice best{256, 1};
-    double least = 1e30;
+    Choice best{256, 1, 1e30};
     auto consider = [&](int kind, int split, double us) {
-        if (us < least) {
-            least = us;
-            best = Choice{kind, split};
-        }
+        if (us < best.us) best = Choice{kind, split, us};
     };
     for (int bn = 128; bn <= 256; bn += 128) {
         const double t = double(pair_tiles(p, bn)), start = bn == 256 ? 6.0 : 4.5, end = (bn == 256 ? 2.5 : 1.9) + (p.e.vec ? 0.0 : bn / 128 * 4.0);
@@ -665,6 +662,8 @@ int64_t product_partial_floats(const Product &p)
     const Choice c = choose(p);
     return c.kind == 0 || c.split == 1 ? 0 : pair_tiles(p, c.kind) * c.split * kPairM * c.kind;
 }
+
+double product_us(const Product &p) { return choose(p).us; }
 
 cudaError_t launch_product(const Product &p, float *partial, cudaStream_t stream)
 {

@@ -371,9 +371,34 @@ __global__ void __launch_bounds__(kThreads) rows_join_kernel(const float *partia
 
 bool aligned(const void *p, int64_t ld, int rows, int size, int to) { return reinterpret_cast<uintptr_t>(p) % to == 0 && (rows == 1 || ld * size % to == 0); }
 
-// The contraction is shared by as many warps as still fit the chip in one go: too few leave its memory idle, and what does not fit
-// runs after the rest.
-// `rows`: rows of x of a block; `group`: weight rows of a warp, over both matrices; `step`: contraction that a warp takes at a time.
+// Whether x and the weights have rows of aligned groups of eight.
+bool eights(const RowsForward &p)
+{
+    const int size = p.e.f32 ? 4 : 2;
+    bool vec = p.in % 8 == 0 && aligned(p.x, p.ldx, p.rows, size, 16);
+    for (int i = 0; i < (p.gated ? 2 : 1); ++i) vec = vec && aligned(p.w[i], p.ldw[i], p.out, size, 16);
+    return vec;
+}
+
+// How a call is cut into blocks.  The contraction is shared by as many warps as still fit the chip in one go: too few leave its memory idle, and what
+// does not fit runs after the rest.
+// `rows`: rows of x of a block; `group`: weight rows of a warp, over both matrices; `step`: contraction that a warp takes at a time; `resident`:
+// blocks that fit the chip.
+struct RowsCut {
+    int slices;
+    int64_t times, across;      // blocks over the rows of x, and over the weight rows
+};
+
+RowsCut cut_rows(const RowsForward &p, int rows, int group, int step, int resident)
+{
+    const int64_t groups = (int64_t(p.out) * (p.gated ? 2 : 1) + group - 1) / group;
+    const int64_t times = (int64_t(p.rows) + rows - 1) / rows;
+    auto across = [=](int slices) { return (groups * slices + kWarps - 1) / kWarps; };
+    int slices = 1;
+    while (slices < kWarps && across(2 * slices) * times <= resident && p.in > step * slices) slices *= 2;
+    return RowsCut{slices, times, across(slices)};
+}
+
 // The kernel is a template argument, not a function argument: all of them have one type, and each has to be asked for its own occupancy, so that
 // the split, and with it the order of the sums, follows from the call alone.  (It is the same on every device that this code runs on.)
 template <void (*KERNEL)(RowsForward)> cudaError_t launch_slices(RowsForward p, int rows, int group, int step, cudaStream_t stream)
@@ -385,15 +410,11 @@ template <void (*KERNEL)(RowsForward)> cudaError_t launch_slices(RowsForward p, 
         if (e != cudaSuccess) return e;
         known = resident *= 148;
     }
-    const int64_t groups = (int64_t(p.out) * (p.gated ? 2 : 1) + group - 1) / group;
-    const int64_t times = (p.rows + rows - 1) / rows;
-    auto blocks = [=](int slices) { return (groups * slices + kWarps - 1) / kWarps * times; };
-    p.slices = 1;
-    while (p.slices < kWarps && blocks(2 * p.slices) <= resident && p.in > step * p.slices) p.slices *= 2;
-    const int64_t count = (groups + kWarps / p.slices - 1) / (kWarps / p.slices);
-    if (count * times > INT32_MAX) return cudaErrorInvalidConfiguration;
-    p.across = int(count);
-    return launch(KERNEL, dim3(unsigned(count * times)), kThreads, 0, 1, stream, p);      // in one dimension: the others end at 65535 blocks
+    const RowsCut cut = cut_rows(p, rows, group, step, resident);
+    if (cut.across * cut.times > INT32_MAX) return cudaErrorInvalidConfiguration;
+    p.slices = cut.slices;
+    p.across = int(cut.across);
+    return launch(KERNEL, dim3(unsigned(cut.across * cut.times)), kThreads, 0, 1, stream, p);      // in one dimension: the others end at 65535 blocks
 }
 
 template <typename T, bool VEC, int R> cudaError_t launch_forward(const RowsForward &p, cudaStream_t stream)
@@ -429,9 +450,7 @@ template <typename T, bool VEC> cudaError_t launch_backward_rows(const RowsBackw
 
 cudaError_t launch_rows_forward(RowsForward p, cudaStream_t stream)
 {
-    const int size = p.e.f32 ? 4 : 2;
-    bool vec = p.in % 8 == 0 && aligned(p.x, p.ldx, p.rows, size, 16);
-    for (int i = 0; i < (p.gated ? 2 : 1); ++i) vec = vec && aligned(p.w[i], p.ldw[i], p.out, size, 16);
+    const bool vec = eights(p);
     if (!p.e.f32 && vec && p.rows > 1) {
         count_launches(1);
         return p.in > 1024 ? launch_mma<8>(p, stream) : launch_mma<4>(p, stream);
@@ -439,6 +458,16 @@ cudaError_t launch_rows_forward(RowsForward p, cudaStream_t stream)
     count_launches(1);
     if (p.e.f32) return vec ? launch_forward_rows<float, true>(p, stream) : launch_forward_rows<float, false>(p, stream);
     return vec ? launch_forward<__nv_bfloat16, true, 1>(p, stream) : launch_forward_rows<__nv_bfloat16, false>(p, stream);
+}
+
+// Blocks of eight rows of x keep 147 registers a thread, one block an SM, so what counts is how often the chip is filled and how many steps of 256 a warp
+// takes each time; rows without vectors load value by value, for as many lanes as there are columns.  Within a third of the measured times of 300
+// calls of 17 to 157 000 rows, widths 1 to 2048 and up to 3e7 weights, counted once for every eight rows.
+double rows_forward_f32_us(const RowsForward &p)
+{
+    const RowsCut cut = cut_rows(p, 8, kWarpRows, 256, 148);
+    const double fills = double((cut.across * cut.times + 147) / 148), steps = double((int64_t(p.in) + 256 * cut.slices - 1) / (256 * cut.slices));
+    return 2.2 + fills * (0.45 + steps * (eights(p) ? 0.8 : 1.0 + 2.2 * std::min(1.0, p.in / 256.0)));
 }
 
 // Weight rows of a strip: about three blocks for every SM, so that the parts of dx stay few.

@@ -34,6 +34,12 @@ KINDS = [("gated_backward", "bf16", "bf16", 1164, 72, 4136), ("gated_backward", 
          ("linear_forward", "bf16", "", 256, 16384, 4096), ("linear_forward", "f32", "", 1458, 25, 1750), ("linear_forward", "f32", "", 26, 2728, 744),
          ("linear_forward", "f32", "", 26, 386, 5734), ("linear_forward", "f32", "", 3073, 1224, 136), ("linear_forward", "f32", "", 100, 2048, 1000)]
 
+# float32 forward products whose work would take the few-row kernel longer: both sides of that rule
+KINDS += [("gated_forward", "f32", "", *s) for s in ((17, 9, 3186), (2966, 11, 18), (3559, 94, 9), (309, 775, 25), (148, 8, 2608), (194, 4180, 24), (130, 8, 4840),
+                                                      (3255, 1112, 72), (100, 2048, 1000), (2000, 64, 64), (24, 704, 1920))]
+KINDS += [("linear_forward", "f32", "", *s) for s in ((34, 9, 5831), (3866, 9, 34), (1232, 314, 9), (1247, 908, 8), (129, 8, 5064), (298, 3358, 28), (387, 8, 5088),
+                                                       (57, 3712, 2408), (8000, 8, 1000), (1000, 64, 1000), (2000, 64, 64), (7000, 1000, 8))]
+
 
 @pytest.mark.parametrize("act", [0, 2])
 @pytest.mark.parametrize("kind", KINDS, ids=str)

@@ -41,3 +41,23 @@ def test_workspaces_count_the_room_to_align_them(op):
     for at in (0, 16):
         assert status(op, large(op, dtype=B.SSD_F32), workspace=BASE + 100 * STEP + at, size=n - 1) == B.SSD_ERR_ARG
         assert status(op, large(op, dtype=B.SSD_F32), workspace=BASE + 100 * STEP + at + 8, size=n + 64) == B.SSD_ERR_ALIGN
+
+
+def room(rows, d, f, op="linear_forward"):
+    a = args_of(op, rows=rows, in_features=d, out_features=f, dtype=B.SSD_F32)
+    for n, t in a._fields_:
+        if n.startswith("ld"):
+            setattr(a, n, d if n in ("ldx", "ldw", "ldwg", "ldwu") else f)
+    st, n = need(op, a)
+    assert st == B.SSD_OK
+    return n
+
+
+def test_which_float32_calls_take_their_operands_apart():
+    """The kernel for a few rows needs no workspace.  It takes small calls; wide, shallow ones of many rows, where it is up to nine times slower, go to
+    the tensor cores, whatever the number of their weights."""
+    for small in ((1, 4096, 4096), (16, 1024, 1024), (64, 512, 512), (24, 1024, 1024), (1024, 64, 10), (1000, 1000, 8), (60, 1000, 1000)):
+        assert room(*small) == 0, small
+    for shallow in ((8000, 8, 1000), (1000, 64, 1000), (1000, 8, 1000), (250, 500, 500), (100000, 1, 64), (1463, 6, 1600), (846, 64, 512)):
+        assert room(*shallow) > 0, shallow
+        assert room(*shallow, op="gated_forward") > 0, shallow
