@@ -291,10 +291,13 @@ void product(Call &c, Product &p)
 //                    1001 x 2003 (rows that lie anywhere), 4 rows 5.7 / 9.9, 8 rows 13 / 9.9; 301 x 200, 30 rows 6.9 / 5.9
 //   float32 forward of more rows, eight at a time: 64 x 512 x 512 4.4 / 9.5, 24 x 1024 x 1024 6.2 / 13.6 (gated 9.9 / 15.4), 1024 x 64 x 10 3.4 / 9.5,
 //                    7000 x 1000 x 8 24 / 30; but 1000 x 64 x 1000 38 / 9.7, 8000 x 8 x 1000 289 / 32, 250 x 500 x 500 30 / 16, 100000 x 1 x 64 240 / 99
+//                    a long contraction or many weights: 8192 x 2048, 8 rows 19 / 14; 32768 x 2048, 8 rows 67 / 29; 2048 x 128256, 16 rows 136 / 103
 //   backward (float32 weight gradients) 4096 x 4096, 8 rows 36 / 54 bfloat16, 39 / 111 float32; 16 rows 51 / 54, 54 / 112;
-//                    256 x 256, 16 rows 6.7 / 16.4 bfloat16
+//                    256 x 256, 16 rows 6.7 / 16.4 bfloat16; 2048 x 128256, 16 rows 717 / 463 bfloat16, 726 / 1302 float32
+//   backward (bfloat16 gradients, 16 rows) 1024 x 1024 17 / 16, 4096 x 4096 50 / 36, 2048 x 128256 722 / 300; 9900 x 7634 (rows off 16 bytes) 370 / 914
 // so multiply-adds take float32 of up to 16 rows, and of more where both sides' estimates say so (over 300 drawn calls 0.4 % slower than the better side of
-// each, 1.4 times at worst), and bfloat16 rows that lie anywhere up to a number of weights, counted once for every eight rows.
+// each, 1.4 times at worst); bfloat16 in aligned rows goes by what a warp has to do (rows_mma_pays: 0.2 % over 110 drawn calls), rows that lie anywhere
+// by the number of weights, counted once for every eight rows.  Backward, nine to sixteen bfloat16 rows go to the tensor cores from a number of weights on.
 constexpr int kFewRowsMost = 16;
 constexpr double kFewEightsAnywhere = 2.5e6;
 
@@ -327,11 +330,17 @@ bool few_rows(const Forward &f)
     const double eights = double((f.rows + 7) / 8) * double(f.out) * double(f.in) * f.mats;      // weights read by eight rows at a time
     bool aligned = tma_can_read(f.x, f.ldx, f.rows, f.dtype) && f.in % 8 == 0;
     for (int i = 0; i < f.mats; ++i) aligned = aligned && tma_can_read(f.w[i], f.ldw[i], f.out, f.dtype);
-    if (aligned) return f.rows <= kFewRowsMost;
+    if (aligned) return f.rows == 1 || (f.rows <= kFewRowsMost && rows_mma_pays(rows_of(f)));
     return f.rows <= 4 ? eights <= kFewEightsAnywhere : f.rows <= 8 && eights <= kFewEightsAnywhere / 8;
 }
 
-bool few_rows(const Backward &b) { return b.rows <= kFewRowsMost; }
+bool few_rows(const Backward &b)
+{
+    if (b.rows <= 8 || b.rows > kFewRowsMost || b.dtype == SSD_F32) return b.rows <= kFewRowsMost;
+    bool aligned = b.in % 8 == 0 && (!b.dw[0] || tma_can_read(b.x, b.ldx, b.rows, b.dtype));
+    for (int i = 0; i < b.mats; ++i) aligned = aligned && (!b.dx || tma_can_read(b.w[i], b.ldw[i], b.out, b.dtype));
+    return !aligned || double(b.out) * double(b.in) * b.mats <= (b.grad_dtype == SSD_F32 ? 5e7 : 5e6);
+}
 
 void run_forward(Call &c, const Forward &f)
 {

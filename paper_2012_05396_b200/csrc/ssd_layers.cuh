@@ -85,6 +85,7 @@ struct RowsBackward {
 
 cudaError_t launch_rows_forward(RowsForward p, cudaStream_t stream);        // these count their launches themselves
 double rows_forward_f32_us(const RowsForward &p);                           // the estimated time for float32 and more than four rows
+bool rows_mma_pays(const RowsForward &p);                                   // bfloat16 in aligned rows, two of them or more: whether these kernels are the faster ones
 int64_t rows_partial_floats(int rows, int out, int in);
 cudaError_t launch_rows_backward(RowsBackward p, cudaStream_t stream);
 

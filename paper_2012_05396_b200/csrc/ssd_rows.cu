@@ -399,6 +399,10 @@ RowsCut cut_rows(const RowsForward &p, int rows, int group, int step, int reside
     return RowsCut{slices, times, across(slices)};
 }
 
+// rows_mma_kernel: weight rows of a warp, blocks that fit the chip, contraction of a step.
+constexpr int kMmaGroup = 16, kMmaResident = 5 * 148;
+int mma_step(const RowsForward &p) { return p.in > 1024 ? 256 : 128; }
+
 // The kernel is a template argument, not a function argument: all of them have one type, and each has to be asked for its own occupancy, so that
 // the split, and with it the order of the sums, follows from the call alone.  (It is the same on every device that this code runs on.)
 template <void (*KERNEL)(RowsForward)> cudaError_t launch_slices(RowsForward p, int rows, int group, int step, cudaStream_t stream)
@@ -425,8 +429,8 @@ template <typename T, bool VEC, int R> cudaError_t launch_forward(const RowsForw
 
 template <int LOADS> cudaError_t launch_mma(const RowsForward &p, cudaStream_t stream)
 {
-    if (p.rows <= 8) return p.gated ? launch_slices<rows_mma_kernel<1, true, LOADS>>(p, 16, 16, 32 * LOADS, stream) : launch_slices<rows_mma_kernel<1, false, LOADS>>(p, 16, 16, 32 * LOADS, stream);
-    return p.gated ? launch_slices<rows_mma_kernel<2, true, LOADS>>(p, 16, 16, 32 * LOADS, stream) : launch_slices<rows_mma_kernel<2, false, LOADS>>(p, 16, 16, 32 * LOADS, stream);
+    if (p.rows <= 8) return p.gated ? launch_slices<rows_mma_kernel<1, true, LOADS>>(p, 16, kMmaGroup, 32 * LOADS, stream) : launch_slices<rows_mma_kernel<1, false, LOADS>>(p, 16, kMmaGroup, 32 * LOADS, stream);
+    return p.gated ? launch_slices<rows_mma_kernel<2, true, LOADS>>(p, 16, kMmaGroup, 32 * LOADS, stream) : launch_slices<rows_mma_kernel<2, false, LOADS>>(p, 16, kMmaGroup, 32 * LOADS, stream);
 }
 
 template <typename T, bool VEC> cudaError_t launch_forward_rows(const RowsForward &p, cudaStream_t stream)
@@ -453,7 +457,7 @@ cudaError_t launch_rows_forward(RowsForward p, cudaStream_t stream)
     const bool vec = eights(p);
     if (!p.e.f32 && vec && p.rows > 1) {
         count_launches(1);
-        return p.in > 1024 ? launch_mma<8>(p, stream) : launch_mma<4>(p, stream);
+        return mma_step(p) == 256 ? launch_mma<8>(p, stream) : launch_mma<4>(p, stream);
     }
     count_launches(1);
     if (p.e.f32) return vec ? launch_forward_rows<float, true>(p, stream) : launch_forward_rows<float, false>(p, stream);
@@ -468,6 +472,15 @@ double rows_forward_f32_us(const RowsForward &p)
     const RowsCut cut = cut_rows(p, 8, kWarpRows, 256, 148);
     const double fills = double((cut.across * cut.times + 147) / 148), steps = double((int64_t(p.in) + 256 * cut.slices - 1) / (256 * cut.slices));
     return 2.2 + fills * (0.45 + steps * (eights(p) ? 0.8 : 1.0 + 2.2 * std::min(1.0, p.in / 256.0)));
+}
+
+// A step of rows_mma_kernel does not hide the way to memory, so few may follow each other: three at most, or any number of them where up to eight
+// rows of x fill two thirds of the chip with blocks.
+bool rows_mma_pays(const RowsForward &p)
+{
+    const RowsCut cut = cut_rows(p, 16, kMmaGroup, mma_step(p), kMmaResident);
+    const int64_t taken = int64_t(mma_step(p)) * cut.slices;
+    return (p.in + taken - 1) / taken <= 3 || (p.rows <= 8 && cut.across >= kMmaResident * 2 / 3);
 }
 
 // Weight rows of a strip: about three blocks for every SM, so that the parts of dx stay few.

@@ -40,6 +40,12 @@ KINDS += [("gated_forward", "f32", "", *s) for s in ((17, 9, 3186), (2966, 11, 1
 KINDS += [("linear_forward", "f32", "", *s) for s in ((34, 9, 5831), (3866, 9, 34), (1232, 314, 9), (1247, 908, 8), (129, 8, 5064), (298, 3358, 28), (387, 8, 5088),
                                                        (57, 3712, 2408), (8000, 8, 1000), (1000, 64, 1000), (2000, 64, 64), (7000, 1000, 8))]
 
+# two to sixteen bfloat16 rows, forward and backward, both sides of where the tensor cores take them
+KINDS += [(op, "bf16", "", *s) for op in ("linear_forward", "gated_forward")
+          for s in ((8, 8192, 520), (2, 20000, 8), (16, 16384, 64), (9, 4112, 1000), (5, 4752, 10304), (16, 3104, 4096), (8, 6152, 129), (3, 6136, 129))]
+KINDS += [(op, "bf16", g, *s) for op in ("linear_backward", "gated_backward") for g in ("f32", "bf16")
+          for s in ((16, 2304, 2304), (9, 2056, 8200), (8, 2304, 2304), (12, 2308, 2304), (16, 8192, 6200), (13, 64, 16384))]
+
 
 @pytest.mark.parametrize("act", [0, 2])
 @pytest.mark.parametrize("kind", KINDS, ids=str)

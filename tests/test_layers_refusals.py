@@ -61,3 +61,25 @@ def test_which_float32_calls_take_their_operands_apart():
     for shallow in ((8000, 8, 1000), (1000, 64, 1000), (1000, 8, 1000), (250, 500, 500), (100000, 1, 64), (1463, 6, 1600), (846, 64, 512)):
         assert room(*shallow) > 0, shallow
         assert room(*shallow, op="gated_forward") > 0, shallow
+
+
+def backward_room(rows, d, f, dtype, grad, op="linear_backward"):
+    a = args_of(op, rows=rows, in_features=d, out_features=f, dtype=dtype, grad_dtype=grad)
+    for n, t in a._fields_:
+        if n.startswith("ld"):
+            setattr(a, n, d if n in ("ldx", "ldw", "ldwg", "ldwu", "lddx", "lddw", "lddwg", "lddwu") else f)
+    st, n = need(op, a)
+    assert st == B.SSD_OK
+    return n
+
+
+def test_room_of_a_few_rows_through_many_weights():
+    """The few-row kernel keeps a part of dx for every strip of weight rows, half a gigabyte for 16 rows of a vocabulary's width; from where the tensor
+    cores are faster, the room does not grow with the weights."""
+    for grad in (B.SSD_F32, B.SSD_BF16):
+        for op in ("linear_backward", "gated_backward"):
+            assert backward_room(16, 4096, 128256, B.SSD_BF16, grad, op) < 1 << 26
+            assert backward_room(9, 32768, 8192, B.SSD_BF16, grad, op) < 1 << 26
+    # small ones keep to it
+    strips = -(-1024 // -(-1024 // 444))
+    assert backward_room(16, 1024, 1024, B.SSD_BF16, B.SSD_F32) < strips * 16 * 1024 * 4 + (1 << 20)
