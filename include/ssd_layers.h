@@ -24,11 +24,13 @@
  *  - Numerics.  Products are summed in float32.  bfloat16 operands enter the tensor cores as they are.
  *    float32 operands enter as three bfloat16 parts of 8 bits each, which hold all 24 bits
  *    (down to steps of 2^-133, bfloat16's smallest: operands below 2^-109 have fewer); of their nine
- *    partial products the six largest are kept, which leaves out less than 2^-22 of |a b| (2^-26 on average).
- *    Up to 16 rows take no parts: float32 multiply-adds, or the tensor cores on bfloat16 as it is.
+ *    partial products the six largest are kept, which leaves out less than 2^-22 of |a b| (2^-26 on average), or the three
+ *    largest where a weight gradient is rounded to bfloat16.  Calls of a few rows, or of little work, take no parts: float32
+ *    multiply-adds, or the tensor cores on bfloat16 as it is.  The tensor cores cut where they add: sums for float32 results are
+ *    therefore rounded to nearest every 512 products; those for bfloat16 results are not, the cuts being below their rounding.
  *    dz = dy * act'(z) is computed in float32 and rounded once to bfloat16 for bfloat16 results, or carried in
- *    three parts (up to 16 rows: in float32) for float32 results.  Epilogues are computed in float32 and rounded
- *    once; gelu's Phi and silu's logistic function to 1e-6.  Results do not depend on timing: the same call gives
+ *    three parts (in calls of a few rows: in float32) for float32 results.  Epilogues are computed in float32 and rounded
+ *    once; gelu's Phi and silu's logistic function to an absolute 1e-6, so that far in their tails few digits are right.  Results do not depend on timing: the same call gives
  *    the same bits.  Which kernel takes a call, and so the order of its sums, depends on its sizes and alignment.
  *    A NaN or infinity in a row of x, or of a weight, reaches the outputs that depend on it (as NaN where float32
  *    operands are split) and no others.
@@ -164,8 +166,8 @@ ssd_status ssd_clip_grad_norm(ssd_grad_list *list, float max_norm, int32_t nonfi
 /* Norms alone: dst is not written. */
 ssd_status ssd_grad_norm(ssd_grad_list *list, float *norms, void *cuda_stream);
 
-/* 1 if a bounded wait inside a layer kernel ever ran out in this process (its results are then incomplete);
- * sticky; the call synchronises the device. */
+/* 1 if a bounded wait inside a layer kernel ever ran out on the current device in this process (its results are then
+ * incomplete); sticky; the call synchronises the device. */
 ssd_status ssd_layer_error(int32_t *flag);
 
 /* Text of the last CUDA error that a call of this header returned as SSD_ERR_CUDA on this host thread. */

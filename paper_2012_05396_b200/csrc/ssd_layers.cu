@@ -246,7 +246,8 @@ Planes operand(Call &c, Passes &passes, const void *src, int64_t ld, int64_t row
 }
 
 // Partial products kept of operands in pa and pb parts (part i is at most 2^-8i of the value): orders 0 to 2, the
-// smallest first.  `half`: orders 0 and 1, for results that are rounded to bfloat16.
+// smallest first; what is left out is 2e-8 of the result's norm, a thirtieth of the rounding of the sums, for six products in place of nine.
+// `half`: orders 0 and 1, for results that are rounded to bfloat16: 3e-6 left out of a result that is rounded to 1.7e-3, for half the products.
 int segments_of(Segment *out, int pa, int pb, int a_step, int b, bool half)
 {
     int n = 0;
@@ -284,16 +285,16 @@ void product(Call &c, Product &p)
     if (c.err == cudaSuccess) c.err = e;
 }
 
-// Which calls go to the kernels for a few rows.  Measured, microseconds there and on the tensor cores:
-//   float32 forward  4096 x 4096, 1 row 13.5 / 60, 8 rows 26 / 60, 16 rows 44 / 61; 1024 x 1024, 16 rows 4.0 / 14
-//   bfloat16 forward 4096 x 4096, 1 row 6.4 / 10, 8 rows 10.6 / 10.6, 16 rows 9.6 / 10.7; 1024 x 1024, 8 rows 2.8 / 5.2;
-//                    gated 2048 x 8192, 8 rows 14.3 / 16.1, 16 rows 16.2 / 16.3
-//                    1001 x 2003 (rows that lie anywhere), 4 rows 5.7 / 9.9, 8 rows 13 / 9.9; 301 x 200, 30 rows 6.9 / 5.9
-//   float32 forward of more rows, eight at a time: 64 x 512 x 512 4.4 / 9.5, 24 x 1024 x 1024 6.2 / 13.6 (gated 9.9 / 15.4), 1024 x 64 x 10 3.4 / 9.5,
+// Which calls go to the kernels for a few rows.  Measured, microseconds there and on the tensor cores, weights from HBM (where they are many enough):
+//   float32 forward  4096 x 4096, 1 row 13.9 / 60, 8 rows 26 / 61, 16 rows 46 / 61; 1024 x 1024, 16 rows 4.8 / 14; 2048 x 128256, 16 rows 514 / 961
+//   float32 forward of more rows, eight at a time: 64 x 512 x 512 4.4 / 9.5, 24 x 1024 x 1024 7.1 / 13.6 (gated 12.2 / 15.4), 1024 x 64 x 10 3.4 / 9.5,
 //                    7000 x 1000 x 8 24 / 30; but 1000 x 64 x 1000 38 / 9.7, 8000 x 8 x 1000 289 / 32, 250 x 500 x 500 30 / 16, 100000 x 1 x 64 240 / 99
+//   bfloat16 forward 4096 x 4096, 1 row 8.3 / 10.4, 8 rows 11.4 / 11.0, 16 rows 10.3 / 11.1; 1024 x 1024, 8 rows 2.7 / 5.2;
+//                    gated 2048 x 8192, 8 rows 14.5 / 16.2, 16 rows 16.5 / 16.8;
 //                    a long contraction or many weights: 8192 x 2048, 8 rows 19 / 14; 32768 x 2048, 8 rows 67 / 29; 2048 x 128256, 16 rows 136 / 103
-//   backward (float32 weight gradients) 4096 x 4096, 8 rows 36 / 54 bfloat16, 39 / 111 float32; 16 rows 51 / 54, 54 / 112;
-//                    256 x 256, 16 rows 6.7 / 16.4 bfloat16; 2048 x 128256, 16 rows 717 / 463 bfloat16, 726 / 1302 float32
+//   ... of rows that lie anywhere (weights in L2): 1001 x 2003, 4 rows 5.7 / 9.9, 8 rows 13 / 9.9; 301 x 200, 30 rows 6.9 / 5.9
+//   backward (float32 weight gradients) 4096 x 4096, 8 rows 35 / 52 bfloat16, 38 / 106 float32; 16 rows 51 / 53, 54 / 108;
+//                    256 x 256, 16 rows 6.6 / 17 bfloat16; 2048 x 128256, 16 rows 717 / 463 bfloat16, 726 / 1302 float32
 //   backward (bfloat16 gradients, 16 rows) 1024 x 1024 17 / 16, 4096 x 4096 50 / 36, 2048 x 128256 722 / 300; 9900 x 7634 (rows off 16 bytes) 370 / 914
 // so multiply-adds take float32 of up to 16 rows, and of more where both sides' estimates say so (over 300 drawn calls 0.4 % slower than the better side of
 // each, 1.4 times at worst); bfloat16 in aligned rows goes by what a warp has to do (rows_mma_pays: 0.2 % over 110 drawn calls), rows that lie anywhere
@@ -414,8 +415,9 @@ void run_backward(Call &c, const Backward &b)
         return;
     }
     const bool plain = b.act == SSD_ACT_NONE && b.mats == 1;      // dz is dy
-    // dz in as many parts as its most exact use asks for: float32 operands, or float32 weight gradients of a
-    // dz that bfloat16 does not hold exactly
+    // dz in as many parts as its most exact use asks for: float32 operands, or float32 weight gradients of a dz that bfloat16 does not hold exactly.
+    // For bfloat16 results one part, a rounding to the type that the results have themselves: two or three parts would take that many times the
+    // products, for an error of 1.7e-3 of the result's norm instead of 2.3e-3 (of which 1.7e-3 is the rounding of the result).
     const int dw_parts = f32 ? 3 : (plain || b.grad_dtype == SSD_BF16 ? 1 : 3);
     const int dx_parts = f32 ? 3 : 1, op_parts = f32 ? 3 : 1;
     const bool dy_ready = plain && tma_can_read(b.dy, b.lddy, b.rows, b.dtype);

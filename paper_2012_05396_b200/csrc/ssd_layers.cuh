@@ -237,7 +237,7 @@ __device__ __forceinline__ void activate_row(float (&v)[32], int act)
 }
 
 // By a whole warp, lane l with row m of its own (`in`: whether there is one); columns n .. n + 31 exist.
-template <bool F32> __device__ __forceinline__ void add_bias_row(const float *bias, int n, float (&v)[32])
+__device__ __forceinline__ void add_bias_row(const float *bias, int n, float (&v)[32])
 {
     if (!bias) return;
     const float b = bias[n + (threadIdx.x & 31)];
@@ -247,11 +247,11 @@ template <bool F32> __device__ __forceinline__ void add_bias_row(const float *bi
 
 template <bool GATED, bool F32> __device__ __forceinline__ void finish_row(const Epilogue &e, int group, bool in, int64_t m, int n, float (&v)[32], float (&u)[32])
 {
-    add_bias_row<F32>(e.bias[0], n, v);
+    add_bias_row(e.bias[0], n, v);
     if (e.z[0] && in) store_row<F32>(e.z[0], m * e.ldz[0] + n, v, e.vec);
     activate_row(v, e.act);
     if (GATED) {
-        add_bias_row<F32>(e.bias[1], n, u);
+        add_bias_row(e.bias[1], n, u);
         if (e.z[1] && in) store_row<F32>(e.z[1], m * e.ldz[1] + n, u, e.vec);
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] *= u[j];

@@ -9,8 +9,8 @@
 // Backward: a block takes a strip of weight rows and kCols columns, four a thread.  dz of the strip is computed first, into shared
 // memory; then one sweep down the strip reads W and writes dW, x staying in registers, and adds up the strip's part of dx, which a
 // second kernel joins over the strips in their order.
-// Measured, 4096 x 4096: forward of 1 row 6.4 us bfloat16 (33.6 MB: 5.1 at the copy rate) and 13.5 float32 (10.3), of 8 rows 10.6 and 26;
-// backward with float32 gradients, 1 row 24 us bfloat16 (15.4), 8 rows 36.
+// Measured, 4096 x 4096, weights from HBM: forward of 1 row 8.0 us bfloat16 (33.6 MB: 5.1 at the copy rate) and 13.7 float32 (10.3), of 8 rows 11.7 and 26;
+// backward with float32 gradients, 1 row 24 us bfloat16 (15.4), 8 rows 35.
 #include "ssd_layers.cuh"
 
 namespace ssd_layers {
@@ -138,7 +138,8 @@ template <typename T, bool VEC, int R, bool GATED> __global__ void __launch_boun
 // A warp multiplies 16 weight rows (gated: 8 of each matrix) with 8 or 16 rows of x.  The order of the contraction is free as long as both
 // operands agree on it, so a thread loads eight consecutive values of its rows and hands them to two instructions as they are.  A step
 // takes 512 bytes of each row, 256 where the contraction is short and more warps have to share it (gated 8 x 2048 x 8192: 14.3 us with 512
-// bytes, 17.4 with 256; 8 x 1024 x 1024: 3.6 and 2.8).
+// bytes, 17.4 with 256; 8 x 1024 x 1024: 3.6 and 2.8).  For up to eight rows both are compiled to 46 registers, so a step's loads are not all under
+// way at once, and a step takes about 4 us from HBM: long contractions are left to the tensor cores (rows_mma_pays).
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -399,7 +400,7 @@ RowsCut cut_rows(const RowsForward &p, int rows, int group, int step, int reside
     return RowsCut{slices, times, across(slices)};
 }
 
-// rows_mma_kernel: weight rows of a warp, blocks that fit the chip, contraction of a step.
+// rows_mma_kernel: weight rows of a warp, blocks that fit the chip (up to eight rows of x: 46 registers a thread), contraction of a step.
 constexpr int kMmaGroup = 16, kMmaResident = 5 * 148;
 int mma_step(const RowsForward &p) { return p.in > 1024 ? 256 : 128; }
 
@@ -464,8 +465,8 @@ cudaError_t launch_rows_forward(RowsForward p, cudaStream_t stream)
     return vec ? launch_forward<__nv_bfloat16, true, 1>(p, stream) : launch_forward_rows<__nv_bfloat16, false>(p, stream);
 }
 
-// Blocks of eight rows of x keep 147 registers a thread, one block an SM, so what counts is how often the chip is filled and how many steps of 256 a warp
-// takes each time; rows without vectors load value by value, for as many lanes as there are columns.  Within a third of the measured times of 300
+// An SM has arithmetic for one block of eight rows of x at a time (its registers hold two), so what counts is how often the chip is filled with those and how
+// many steps of 256 a warp takes each time; rows without vectors load value by value, for as many lanes as there are columns.  Within a third of the measured times of 300
 // calls of 17 to 157 000 rows, widths 1 to 2048 and up to 3e7 weights, counted once for every eight rows.
 double rows_forward_f32_us(const RowsForward &p)
 {

@@ -10,6 +10,9 @@ comes from torch's caching allocator on the stream that the call runs on.
 
 Activations x, y, z, ... may have leading dimensions that flatten to rows; weights are [out, in] as
 torch.nn.Linear has them.  The last dimension is contiguous, rows may be strided.
+
+Autograd does not see these calls: inputs that require gradients are taken as they are, and outputs have no history.  Gradients come from the
+backward calls.
 """
 from __future__ import annotations
 
@@ -167,7 +170,11 @@ class GradList:
     """The tensors that are clipped together, made once for buffers that are used again and again.
 
     grads: contiguous tensors of one type; out: where the clipped gradients go (None = in place); groups: the
-    group of every tensor, ascending (None = one group); e.g. a worker's arena each, with groups=range(K)."""
+    group of every tensor, ascending (None = one group); e.g. a worker's arena each, with groups=range(K).
+
+    Making one costs about a microsecond of host time a tensor and waits for the copy of its table: worth it for arenas that live as long as
+    the training, not for gradients that are allocated anew each step.  A list outlives the CUDA graphs that its calls were captured into.
+    Calls on one list must not overlap on the GPU; they may run on any stream."""
 
     def __init__(self, grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None,
                  groups: Optional[Sequence[int]] = None, num_groups: Optional[int] = None, stream=None):
