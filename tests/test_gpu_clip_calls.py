@@ -132,3 +132,24 @@ def test_norms_over_what_a_call_uses_are_refused():
     for norms in (arena[1022:1024], arena[2048:2050], arena[3070:3072], arena[:2], arena[4000:4002], push[1024:1026], push[2046:2048], push[2976:2978]):
         assert L.ssd_clip_grad_norm(lst, 1.0, norms=norms) is not None
         assert torch.allclose(norms, torch.tensor(want, device="cuda"), rtol=1e-6)
+
+
+def test_a_list_made_while_its_stream_is_captured():
+    """Its table is filled when the graph runs, before the calls that the graph holds, with other kernels between them."""
+    g, norms = torch.empty(70000, device="cuda"), torch.zeros(2, device="cuda")
+    g.fill_(1.0)
+    L.ssd_clip_grad_norm(L.GradList([g[:50000], g[50000:]], groups=[0, 1]), 1e9, norms=norms)      # the kernels are known to the device
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lst = L.GradList([g[:50000], g[50000:]], groups=[0, 1])
+        g.mul_(2.0)
+        L.ssd_clip_grad_norm(lst, 100.0, norms=norms)
+    for v in (0.25, 1.0, 3.0):
+        g.fill_(v)
+        graph.replay()
+        want = [2 * v * 50000 ** 0.5, 2 * v * 20000 ** 0.5]
+        assert torch.allclose(norms, torch.tensor(want, device="cuda"), rtol=1e-6)
+        for part, n in ((g[:50000], want[0]), (g[50000:], want[1])):
+            assert torch.allclose(part, torch.full_like(part, 2 * v * min(1.0, 100.0 / (n + 1e-6))), rtol=1e-6)
+    torch.cuda.synchronize()
+    del graph, lst
